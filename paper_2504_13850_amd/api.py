@@ -29,12 +29,15 @@ EXPORTS = [
     "fo_set_graph_mode", "fo_gemm_bf16", "fo_conv2d_bf16", "fo_conv2d_bf16_ordered", "fo_gemm_bf16_noalloc",
     "fo_queues_push_batch", "fo_queues_push_model_batch", "fo_device_step", "fo_queues_set_policy", "fo_queues_set_device_active",
     "fo_queues_sender_status", "fo_queues_log_enable", "fo_queues_log_read", "fo_pipeline_run",
-    "fo_net_units", "fo_select_split", "fo_aux_network",
+    "fo_net_units", "fo_select_split", "fo_aux_network", "fo_attn_workspace", "fo_attn_fwd", "fo_attn_bwd",
+    "fo_relpos_buckets", "fo_dropout_fwd", "fo_dropout_workspace", "fo_dropout_bwd",
 ]
 FO_NET_VGG5, FO_NET_MOBILENETV3_LARGE, FO_NET_TRANSFORMER6, FO_NET_TRANSFORMER12, FO_NET_VGG16 = range(1, 6)
 FO_SCHED_COUNTER, FO_SCHED_FIFO = 0, 1
 FO_EV_PUSH, FO_EV_MODEL, FO_EV_PICK, FO_EV_RELEASE, FO_EV_AGG, FO_EV_LEAVE, FO_EV_JOIN = range(1, 8)
 FO_LAYOUT_ROW_K, FO_LAYOUT_K_ROW = 0, 1
+FO_DT_BF16, FO_DT_F32 = 0, 1
+FO_ATTN_FULL, FO_ATTN_CAUSAL, FO_ATTN_PREFIX = range(3)
 
 
 class FoError(RuntimeError):
@@ -87,6 +90,17 @@ class fo_pipeline_stats(C.Structure):
                 ("samples", C.c_int64), ("aggregations", C.c_int64), ("skipped", C.c_int64), ("sent", C.c_int64),
                 ("not_sent", C.c_int64), ("models_sent", C.c_int64), ("leaves", C.c_int64), ("rejoins", C.c_int64),
                 ("device_iterations", C.c_int64)]
+
+
+class fo_attn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("max_q", C.c_int32), ("max_k", C.c_int32), ("q_rows", C.c_int64),
+                ("k_rows", C.c_int64), ("q_begin", C.c_void_p), ("q_end", C.c_void_p), ("k_begin", C.c_void_p),
+                ("k_end", C.c_void_p), ("q_ld", C.c_int64), ("q_hs", C.c_int64), ("k_ld", C.c_int64),
+                ("k_hs", C.c_int64), ("v_ld", C.c_int64), ("v_hs", C.c_int64), ("out_ld", C.c_int64),
+                ("out_hs", C.c_int64), ("scale", C.c_float), ("cap", C.c_float), ("mask", C.c_int32),
+                ("prefix", C.c_void_p), ("table", C.c_void_p), ("bucket", C.c_void_p), ("n_buckets", C.c_int32),
+                ("radius", C.c_int32), ("p", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint32)]
 
 
 _lib = None
@@ -154,6 +168,15 @@ def lib():
                                                  vp, C.POINTER(i32), vp]),
             "fo_gemm_bf16_noalloc": (C.c_int, [i32, i32, i32, i32, vp, vp, i64, i32, vp, vp, i64, vp, i64, i32,
                                                vp]),
+            "fo_attn_workspace": (i64, [C.POINTER(fo_attn), i32]),
+            "fo_attn_fwd": (C.c_int, [C.POINTER(fo_attn), vp, vp, vp, vp, vp, vp, i64, vp]),
+            "fo_attn_bwd": (C.c_int, [C.POINTER(fo_attn), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
+            "fo_relpos_buckets": (C.c_int, [i32, i32, i32, vp]),
+            "fo_dropout_fwd": (C.c_int, [i32, i64, i32, vp, i64, vp, vp, i64, f32, C.c_uint64, C.c_uint32, vp, i64,
+                                         vp]),
+            "fo_dropout_workspace": (i64, [i64, i32]),
+            "fo_dropout_bwd": (C.c_int, [i32, i64, i32, vp, i64, f32, C.c_uint64, C.c_uint32, vp, i64, vp, vp, i64,
+                                         vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -490,3 +513,116 @@ def fo_conv2d_bf16_ordered(pass_, Bn, H, W, Ci, Co, k, stride, pad, inp, inp_lo,
                                         _dptr(w_lo), _dptr(out), splits, _dptr(workspace),
                                         C.byref(left) if keep_slices else None, _stream(stream)))
     return left.value
+
+
+# ------------------------------------------------------------------ transformer operators
+def _dtype(t) -> int:
+    """FO_DT_* of a tensor (bfloat16, or float32)."""
+    size = t.element_size()
+    if not t.is_floating_point() or size not in (2, 4) or (size == 2 and "bfloat16" not in str(t.dtype)):
+        raise FoError(FO_EINVAL, f"bfloat16 or float32 operands, not {t.dtype}")
+    return FO_DT_BF16 if size == 2 else FO_DT_F32
+
+
+def _same(what, ref, *tensors):
+    """The given tensors (None apart) have ref's type, and their last dimension is contiguous."""
+    for t in tensors:
+        if t is not None and (t.dtype != ref.dtype or (t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1)):
+            raise FoError(FO_EINVAL, f"{what}: operands of one type with a contiguous last dimension")
+
+
+def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: int, scale=None, cap: float = 0.0,
+              mask: int = FO_ATTN_FULL, prefix=None, table=None, bucket=None, p: float = 0.0, seed: int = 0,
+              offset: int = 0) -> fo_attn:
+    """The record of an attention over q [rows, heads, dim], k and v [rows, kv_heads, dim] and out like q, whose
+    rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  The record holds addresses: the bounds,
+    prefix, table and bucket tensors have to live until the calls that use it have run."""
+    rows, heads, dim = q.shape
+    k_rows, kv_heads, _ = k.shape
+    if k.shape[2] != dim or v.shape != k.shape or out.shape != q.shape:
+        raise FoError(FO_EINVAL, f"fo_attn: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, "
+                                 f"out {tuple(out.shape)}")
+    _same("fo_attn", q, q, k, v, out, table)
+    batch = q_begin.numel()
+    for t, n in ((q_begin, batch), (q_end, batch), (k_begin, batch), (k_end, batch), (prefix, batch), (bucket, None)):
+        if t is not None and ("int32" not in str(t.dtype) or not t.is_contiguous() or t.numel() != (n or t.numel())):
+            raise FoError(FO_EINVAL, "fo_attn: sequence bounds, prefix and bucket are int32, one bound per sequence")
+    if table is not None and (table.dim() != 2 or table.shape[1] != heads or not table.is_contiguous()
+                              or bucket is None or bucket.numel() % 2 == 0):
+        raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the buckets of 2 radius + 1 distances")
+    (ql, qh, _), (kl, kh, _), (vl, vh, _), (ol, oh, _) = q.stride(), k.stride(), v.stride(), out.stride()
+    return fo_attn(_dtype(q), batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(),
+                   q_end.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh,
+                   dim ** -0.5 if scale is None else scale, cap, mask, _dptr(prefix), _dptr(table), _dptr(bucket),
+                   0 if table is None else table.shape[0], 0 if table is None else bucket.numel() // 2, p, seed,
+                   offset)
+
+
+def _bytes(ws) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def fo_attn_workspace(attn: fo_attn, backward: bool = False) -> int:
+    """Bytes of workspace for fo_attn_fwd, or for both calls."""
+    n = lib().fo_attn_workspace(C.byref(attn), 1 if backward else 0)
+    if n < 0:
+        raise FoError(FO_EINVAL, last_error())
+    return n
+
+
+def fo_attn_fwd(attn: fo_attn, q, k, v, out, lse=None, workspace=None, stream=None):
+    _check(lib().fo_attn_fwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
+                             _dptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_attn_bwd(attn: fo_attn, q, k, v, out, lse, dout, dq, dk, dv, dtable=None, workspace=None, stream=None):
+    """dout has out's strides; dq, dk and dv have those of q, k and v."""
+    _same("fo_attn_bwd", q, dout, dq, dk, dv, dtable)
+    for a, b in ((out, dout), (q, dq), (k, dk), (v, dv)):
+        if a.shape != b.shape or any(n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride())):
+            raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the shapes and strides of what they belong to")
+    if dtable is not None and (not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
+        raise FoError(FO_EINVAL, "fo_attn_bwd: dtable has the table's shape")
+    _check(lib().fo_attn_bwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
+                             dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _dptr(dtable),
+                             _dptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_relpos_buckets(n_buckets: int, radius: int, causal: bool = False) -> np.ndarray:
+    """The bucket of each distance -radius..radius, int32[2 radius + 1]."""
+    out = np.empty(2 * max(radius, 0) + 1, np.int32)
+    _check(lib().fo_relpos_buckets(n_buckets, radius, 1 if causal else 0, out.ctypes.data))
+    return out
+
+
+def fo_dropout_fwd(x, y, p: float, seed: int, offset: int, bias=None, residual=None, stream=None):
+    """y = drop(x + bias) + residual on [rows, cols] matrices with any row strides."""
+    _same("fo_dropout_fwd", x, x, y, bias, residual)
+    rows, cols = x.shape
+    if y.shape != x.shape or (residual is not None and residual.shape != x.shape) or (
+            bias is not None and bias.numel() != cols):
+        raise FoError(FO_EINVAL, "fo_dropout_fwd: shapes differ")
+    _check(lib().fo_dropout_fwd(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _dptr(bias), _dptr(residual),
+                                0 if residual is None else _ld(residual), p, seed, offset, y.data_ptr(), _ld(y),
+                                _stream(stream)))
+
+
+def _ld(t) -> int:
+    """Row stride of a matrix; a single row's is its width, whatever torch keeps there."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def fo_dropout_workspace(rows: int, cols: int) -> int:
+    n = lib().fo_dropout_workspace(rows, cols)
+    if n < 0:
+        raise FoError(FO_EINVAL, last_error())
+    return n
+
+
+def fo_dropout_bwd(dy, dx, p: float, seed: int, offset: int, dbias=None, workspace=None, stream=None):
+    _same("fo_dropout_bwd", dy, dy, dx, dbias)
+    rows, cols = dy.shape
+    if dx.shape != dy.shape or (dbias is not None and dbias.numel() != cols):
+        raise FoError(FO_EINVAL, "fo_dropout_bwd: shapes differ")
+    _check(lib().fo_dropout_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), p, seed, offset, dx.data_ptr(),
+                                _ld(dx), _dptr(dbias), _dptr(workspace), _bytes(workspace), _stream(stream)))
