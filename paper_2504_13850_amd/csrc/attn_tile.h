@@ -1,0 +1,260 @@
+// Matrix-core building blocks of the attention operators: 32x32 products,
+// LDS tiles and their operand fragments, and what a score is made of.
+//
+// Transposed orientation: a wave owns 32 rows (queries, or keys in the key
+// kernel) which sit on the accumulator columns, one row per lane pair (l, l +
+// 32).  Accumulator register r of lane l is column-of-the-other-side
+//   8 (r / 4) + 4 (l / 32) + r % 4,
+// so statistics over the other side reduce within a lane plus one exchange
+// between the half-waves, and 16 of a tile's 32 entries (registers 8 kb .. 8 kb
+// + 7) already are the B operand of a product that sums over them, provided the
+// A operand takes its k index in the same order (frag_col).
+#pragma once
+
+#include "ops.h"
+
+namespace fo {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// An operand of one step of 16 k values: lane l holds row l % 32 and k = 8 (l / 32) + e, e = 0..7.
+template <class T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+    bf16x8_t v;
+};
+template <>
+struct Frag<float> {
+    float v[8];
+};
+
+// c += A B over 16 k values.  fp32 takes eight 32x32x2 products, the e-th over k = e and 8 + e.
+__device__ __forceinline__ f32x16 mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+    return c;
+}
+
+// Eight accumulator values as an operand (one rounding to bf16).
+template <class T>
+__device__ __forceinline__ Frag<T> pack8(const float* x);
+template <>
+__device__ __forceinline__ Frag<bf16_t> pack8<bf16_t>(const float* x) {
+    const u32x4_t u = {f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])};
+    return {__builtin_bit_cast(bf16x8_t, u)};
+}
+template <>
+__device__ __forceinline__ Frag<float> pack8<float>(const float* x) {
+    Frag<float> f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = x[e];
+    return f;
+}
+
+// An LDS tile of rows of DP values.  bf16: 16-byte chunks XOR-swizzled by row so
+// that neither the row reads (16 rows, one chunk each) nor the transpose reads
+// (four consecutive rows of 64 bytes) share banks.  fp32: rows padded by one
+// 16-byte chunk, which spreads the row reads; column reads are consecutive.
+template <class T, int DP>
+struct Tile;
+template <int DP>
+struct Tile<bf16_t, DP> {
+    static constexpr int LD = DP, CHUNK = 8;
+    static __device__ __forceinline__ int idx(int row, int col) {
+        int x;
+        if (DP == 128) x = ((row & 3) << 2) | ((row >> 2) & 3);
+        else if (DP == 64) x = (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        else x = (row >> 2) & 3;
+        return row * DP + ((((col >> 3) ^ x) << 3) | (col & 7));
+    }
+    // Lane rows are tile rows row0 + l % 32, k runs along the row.
+    static __device__ __forceinline__ Frag<bf16_t> frag_row(const bf16_t* t, int row0, int col0, int lane) {
+        return {*reinterpret_cast<const bf16x8_t*>(&t[idx(row0 + (lane & 31), col0 + 8 * (lane >> 5))])};
+    }
+    // Lane rows are tile columns col0 + l % 32, k are 16 tile rows from row0 in the
+    // accumulators' order: two transpose reads (ds_read_b64_tr_b16: within each group
+    // of 16 lanes, lane i receives element i mod 4 of the 8 bytes addressed by lane
+    // 4 j + i / 4, j = 0..3).
+    static __device__ __forceinline__ Frag<bf16_t> frag_col(const bf16_t* t, int row0, int col0, int lane) {
+        const int g = lane >> 4, s = lane & 15, col = col0 + 16 * (g & 1) + 4 * (s & 3);
+        s16x4_t v[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            v[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4_t*)(t + idx(row0 + 4 * (lane >> 5) + 8 * r + (s >> 2), col)));
+        const s16x8_t o = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+        return {__builtin_bit_cast(bf16x8_t, o)};
+    }
+};
+template <int DP>
+struct Tile<float, DP> {
+    static constexpr int LD = DP + 4, CHUNK = 4;
+    static __device__ __forceinline__ int idx(int row, int col) { return row * LD + col; }
+    static __device__ __forceinline__ Frag<float> frag_row(const float* t, int row0, int col0, int lane) {
+        const f32x4* p = reinterpret_cast<const f32x4*>(&t[idx(row0 + (lane & 31), col0 + 8 * (lane >> 5))]);
+        const f32x4 a = p[0], b = p[1];
+        return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+    }
+    static __device__ __forceinline__ Frag<float> frag_col(const float* t, int row0, int col0, int lane) {
+        Frag<float> f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            f.v[e] = t[idx(row0 + 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2), col0 + (lane & 31))];
+        return f;
+    }
+};
+
+// 16 bytes of a row from column d on, zeros past D or where !ok.  vec: every row
+// starts 16-byte aligned and D is a whole number of chunks; else element by element.
+template <class T>
+__device__ __forceinline__ uint4 ld_chunk(const T* row, int d, int D, bool ok, bool vec) {
+    constexpr int N = 16 / sizeof(T);
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (vec) {
+        if (ok && d < D) u = *reinterpret_cast<const uint4*>(row + d);
+        return u;
+    }
+    T v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = ok && d + e < D ? row[d + e] : T(0);
+    __builtin_memcpy(&u, v, 16);
+    return u;
+}
+template <class T>
+__device__ __forceinline__ Frag<T> ld_frag(const T* row, int d, int D, bool ok, bool vec) {
+    Frag<T> f;
+#pragma unroll
+    for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
+        const uint4 u = ld_chunk(row, d + c * (16 / (int)sizeof(T)), D, ok, vec);
+        __builtin_memcpy((char*)&f.v + 16 * c, &u, 16);
+    }
+    return f;
+}
+
+// ROWS rows of a [rows][ld] operand through registers into an LDS tile: 256
+// threads, all loads of a tile issued together so that they fly while the
+// previous tile is in use.
+template <class T, int DP, int ROWS>
+struct Stage {
+    static constexpr int CPR = DP * (int)sizeof(T) / 16, N = ROWS * CPR / 256, EPC = 16 / (int)sizeof(T);
+    static_assert(ROWS * CPR % 256 == 0, "whole chunks per thread");
+    uint4 u[N];
+    // Rows r0 .. of which those below n exist.
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int r0, int n, int D, bool vec, int tid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = tid + 256 * i, r = r0 + x / CPR;
+            u[i] = ld_chunk(base + (int64_t)r * ld, (x % CPR) * EPC, D, r < n, vec);
+        }
+    }
+    __device__ __forceinline__ void store(T* t, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = tid + 256 * i;
+            *reinterpret_cast<uint4*>(&t[Tile<T, DP>::idx(x / CPR, (x % CPR) * EPC)]) = u[i];
+        }
+    }
+};
+
+// A row's DP accumulated values times s: register 4 q + e of accumulator t is column 32 t + 8 q + 4 (l / 32) + e.
+template <class T, int DP>
+__device__ __forceinline__ void store_row(T* row, const f32x16* acc, float s, int lh, int D, bool vec) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = 32 * t + 8 * q + 4 * lh;
+            const float v[4] = {acc[t][4 * q] * s, acc[t][4 * q + 1] * s, acc[t][4 * q + 2] * s, acc[t][4 * q + 3] * s};
+            if (vec) {
+                if (c >= D) continue;
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<uint2*>(row + c) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
+                else
+                    *reinterpret_cast<f32x4*>(row + c) = f32x4{v[0], v[1], v[2], v[3]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < D) row[c + e] = from_f<T>(v[e]);
+            }
+        }
+}
+
+// ------------------------------------------------------------------ scores, base 2
+// u log2(e) = S mul + add, or with a cap cl (1 - 2 w) + add, w = 1 / (e^(2 s / cap) + 1)
+// and s = scale S: tanh(x) = 1 - 2 / (e^2x + 1), whose absolute error of some 2^-23 is
+// far below a bf16 probability's rounding.  fp32 calls tanhf.
+struct ScoreK {
+    float mul;   // scale log2(e)
+    float ck;    // 2 scale log2(e) / cap
+    float cs;    // scale / cap
+    float cl;    // cap log2(e)
+};
+__device__ __forceinline__ ScoreK score_k(const fo_attn& a) {
+    ScoreK k;
+    k.mul = a.scale * kLog2e;
+    k.cs = a.cap > 0.f ? a.scale / a.cap : 0.f;
+    k.ck = 2.f * kLog2e * k.cs;
+    k.cl = a.cap * kLog2e;
+    return k;
+}
+// The capped score without its bias; slope = du / ds.
+template <class T>
+__device__ __forceinline__ float capped(float S, const ScoreK& k, float* slope = nullptr) {
+    if constexpr (sizeof(T) == 2) {
+        const float w = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(S * k.ck) + 1.f);
+        if (slope) *slope = 4.f * fmaf(-w, w, w);
+        return fmaf(w, -2.f * k.cl, k.cl);
+    } else {
+        const float t = tanhf(S * k.cs);
+        if (slope) *slope = fmaf(-t, t, 1.f);
+        return t * k.cl;
+    }
+}
+
+// The bias of distance n (clamped to the radius) in base 2; -infinity where it hides.
+template <class T>
+__device__ __forceinline__ float bias_at(const fo_attn& a, int h, int n) {
+    const int g = min(max(a.bucket[min(max(n, -a.radius), a.radius) + a.radius], 0), a.n_buckets - 1);
+    const float t = to_f(((const T*)a.table)[(int64_t)g * a.heads + h]);
+    return t <= -1e30f ? -INFINITY : t * kLog2e;
+}
+// Distances of a 32-row by up to 64-column tile reach at most kReach past the
+// radius before the whole tile lies beyond it, where its bias is one value.
+constexpr int kReach = 96;
+__host__ __device__ inline int lut_floats(const fo_attn& a) { return 2 * (a.radius + kReach) + 1; }
+template <class T>
+__device__ __forceinline__ void fill_lut(float* lut, const fo_attn& a, int h, int tid) {
+    for (int x = tid; x < lut_floats(a); x += 256) lut[x] = bias_at<T>(a, h, x - a.radius - kReach);
+}
+
+// One past the last key that query i sees: a prefix of the keys for every mask.
+__device__ __forceinline__ int limit_of(const fo_attn& a, const Span& s, int pre, int i) {
+    if (a.mask == FO_ATTN_FULL) return s.nk;
+    return max(0, min(max(i + (s.nk - s.nq) + 1, pre), s.nk));
+}
+
+// keep factors of the 16 keys of a 32-key subtile from key j0 (a multiple of 32)
+// on that this lane holds for query i: two generator calls.
+__device__ __forceinline__ uint32_t keep_bits(uint32_t thr, int j0, int lh, int i, int bh, const fo_attn& a) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const uint4 w = philox7(2 * ((j0 >> 4) + m) + lh, i, bh, a.offset, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bits |= (half_of(w, e) >= thr ? 1u : 0u) << (8 * m + e);
+    }
+    return bits;
+}
+
+}  // namespace fo
