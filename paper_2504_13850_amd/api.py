@@ -516,18 +516,26 @@ def fo_conv2d_bf16_ordered(pass_, Bn, H, W, Ci, Co, k, stride, pad, inp, inp_lo,
 
 
 # ------------------------------------------------------------------ transformer operators
+_DTYPES, _INT32 = {}, []  # torch.dtype -> FO_DT_*; torch.int32 (torch is imported on first use)
+
+
 def _dtype(t) -> int:
-    """FO_DT_* of a tensor (bfloat16, or float32)."""
-    size = t.element_size()
-    if not t.is_floating_point() or size not in (2, 4) or (size == 2 and "bfloat16" not in str(t.dtype)):
+    """FO_DT_* of a tensor."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: FO_DT_BF16, torch.float32: FO_DT_F32})
+        _INT32.append(torch.int32)
+    got = _DTYPES.get(t.dtype)
+    if got is None:
         raise FoError(FO_EINVAL, f"bfloat16 or float32 operands, not {t.dtype}")
-    return FO_DT_BF16 if size == 2 else FO_DT_F32
+    return got
 
 
 def _same(what, ref, *tensors):
     """The given tensors (None apart) have ref's type, and their last dimension is contiguous."""
+    dt = ref.dtype
     for t in tensors:
-        if t is not None and (t.dtype != ref.dtype or (t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1)):
+        if t is not None and (t.dtype != dt or (t.stride(-1) != 1 and t.shape[-1] > 1)):
             raise FoError(FO_EINVAL, f"{what}: operands of one type with a contiguous last dimension")
 
 
@@ -537,25 +545,28 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
     """The record of an attention over q [rows, heads, dim], k and v [rows, kv_heads, dim] and out like q, whose
     rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  The record holds addresses: the bounds,
     prefix, table and bucket tensors have to live until the calls that use it have run."""
-    rows, heads, dim = q.shape
-    k_rows, kv_heads, _ = k.shape
-    if k.shape[2] != dim or v.shape != k.shape or out.shape != q.shape:
-        raise FoError(FO_EINVAL, f"fo_attn: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, "
+    dt, batch = _dtype(q), q_begin.numel()
+    rows, heads, dim = shape = q.shape
+    k_rows, kv_heads, k_dim = k_shape = k.shape
+    if k_dim != dim or v.shape != k_shape or out.shape != shape:
+        raise FoError(FO_EINVAL, f"fo_attn: q {tuple(shape)}, k {tuple(k_shape)}, v {tuple(v.shape)}, "
                                  f"out {tuple(out.shape)}")
     _same("fo_attn", q, q, k, v, out, table)
-    batch = q_begin.numel()
-    for t, n in ((q_begin, batch), (q_end, batch), (k_begin, batch), (k_end, batch), (prefix, batch), (bucket, None)):
-        if t is not None and ("int32" not in str(t.dtype) or not t.is_contiguous() or t.numel() != (n or t.numel())):
-            raise FoError(FO_EINVAL, "fo_attn: sequence bounds, prefix and bucket are int32, one bound per sequence")
-    if table is not None and (table.dim() != 2 or table.shape[1] != heads or not table.is_contiguous()
-                              or bucket is None or bucket.numel() % 2 == 0):
-        raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the buckets of 2 radius + 1 distances")
+    for t in (q_begin, q_end, k_begin, k_end, prefix):
+        if t is not None and (t.dtype != _INT32[0] or t.numel() != batch or (batch > 1 and t.stride() != (1,))):
+            raise FoError(FO_EINVAL, "fo_attn: sequence bounds and prefix are int32, one for each sequence")
+    n_buckets = radius = 0
+    if table is not None:
+        n_buckets, radius = table.shape[0], 0 if bucket is None else bucket.numel() // 2
+        if (table.shape[1:] != (heads,) or not table.is_contiguous() or bucket is None or bucket.numel() % 2 == 0
+                or bucket.dtype != _INT32[0] or not bucket.is_contiguous()):
+            raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the int32 buckets of 2 radius + 1 "
+                                     "distances")
     (ql, qh, _), (kl, kh, _), (vl, vh, _), (ol, oh, _) = q.stride(), k.stride(), v.stride(), out.stride()
-    return fo_attn(_dtype(q), batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(),
+    return fo_attn(dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(),
                    q_end.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh,
                    dim ** -0.5 if scale is None else scale, cap, mask, _dptr(prefix), _dptr(table), _dptr(bucket),
-                   0 if table is None else table.shape[0], 0 if table is None else bucket.numel() // 2, p, seed,
-                   offset)
+                   n_buckets, radius, p, seed, offset)
 
 
 def _bytes(ws) -> int:
