@@ -25,7 +25,23 @@ struct BwdShape {
 template <class T, int DP>
 constexpr int min_wk() { return sizeof(T) == 4 && DP == 128 ? 2 : 1; }
 
+// Workgroups per compute unit that the registers are held to.
+template <class T, int DP>
+constexpr int bwd_occ() { return sizeof(T) == 4 || DP == 128 ? 1 : 2; }
+
 constexpr int bwd_kb(int wn) { return wn == 4 ? 64 : 32 * (4 / wn); }
+
+// Scores S -> u log2(e) + add, and du/ds.
+template <class T, bool CAP>
+__device__ __forceinline__ void to_exponent(f32x16& S, float* slope, const ScoreK& k, float add) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[r] = CAP ? capped<T>(S[r], k, &slope[r]) + add : fmaf(S[r], k.mul, add);
+}
+template <class F>
+__device__ __forceinline__ void near_bias(f32x16& S, F f) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) S[r] += f(r);
+}
 
 // dq and delta.  bf16: delta is first taken as dO.out, whose rounding (2^-9 of
 // out) would be the largest error of the gradients.  dU then misses delta's error
@@ -33,8 +49,8 @@ constexpr int bwd_kb(int wn) { return wn == 4 ? 64 : 32 * (4 / wn); }
 // kernel also sums X_i = sum_j P_ij du/ds k_j and subtracts e_i X_i: one more
 // product instead of a pass for delta, which would take two and the
 // exponentials again.
-template <class T, int DP, int WQ, bool CAP>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn_dq_kernel(AttnArgs x, BwdShape f) {
+template <class T, int DP, int WQ, bool CAP, bool EXTRA>
+__global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnArgs x, BwdShape f) {
     constexpr int WK = 4 / WQ, KB = bwd_kb(WQ), KT = KB / 32 / WK, NK = DP / 16, ND = DP / 32;
     constexpr bool FIX = sizeof(T) == 2;
     using TL = Tile<T, DP>;
@@ -91,7 +107,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
     float lse = ok ? x.lse[stat] : INFINITY;
     if (lse == -INFINITY) lse = INFINITY;  // a row that sees nothing: every P is exp2(-inf) = 0
     const ScoreK sc = score_k(a);
-    const bool bias = a.table != nullptr;
+    const bool bias = EXTRA && a.table != nullptr;
     float far_lo = 0.f, far_hi = 0.f;
     if (bias) {
         far_lo = bias_at<T>(a, h, -a.radius);
@@ -126,28 +142,33 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
                 S = mma(TL::frag_row(Ks, kw, 16 * kk, lane), q[kk], S);
                 G = mma(TL::frag_row(Vs, kw, 16 * kk, lane), g[kk], G);
             }
+            float slope[16];
             const int n_lo = j0 - (iw + 31) - off, n_hi = j0 + 31 - iw - off;
-            const bool near = bias && n_lo < a.radius && n_hi > -a.radius;
-            const float add0 = !bias ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
-            const int base = j0 + 4 * lh - qi - off + a.radius + kReach;
-            const bool masked = j0 + 32 > wave_all;
-            const int left = lim - j0 - 4 * lh;
-            uint32_t bits = 0xFFFFu;
-            if (x.thr) bits = keep_bits(x.thr, j0, lh, qi, b * a.heads + h, a);
+            const bool near = EXTRA && bias && n_lo < a.radius && n_hi > -a.radius;
+            const float add0 = !bias || near ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
+            to_exponent<T, CAP>(S, slope, sc, add0 - lse);
+            if (near) {
+                const float* at = &lut[j0 + 4 * lh - qi - off + a.radius + kReach];
+                near_bias(S, [&](int r) { return at[8 * (r >> 2) + (r & 3)]; });
+            }
+            if (j0 + 32 > wave_all) {
+                const int left = lim - j0 - 4 * lh;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (8 * (r >> 2) + (r & 3) >= left) S[r] = -INFINITY;
+            }
+            if (EXTRA && x.thr) {
+                const uint32_t bits = keep_bits(x.thr, j0, lh, qi, b * a.heads + h, a);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) G[r] = (bits >> r) & 1 ? G[r] * x.keep_scale : 0.f;
+            }
             float ds[16], ps[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int j = 8 * (r >> 2) + (r & 3);
-                float slope = 1.f;
-                const float add = near ? lut[base + j] : add0;
-                const float u = CAP ? capped<T>(S[r], sc, &slope) + add : fmaf(S[r], sc.mul, add);
-                float p = __builtin_amdgcn_exp2f(u - lse);
-                if (masked) p = j < left ? p : 0.f;
-                const float dp = x.thr ? ((bits >> r) & 1 ? G[r] * x.keep_scale : 0.f) : G[r];
-                const float du = p * (dp - dl);
+                const float p = __builtin_amdgcn_exp2f(S[r]), du = p * (G[r] - dl);
                 err += du;
-                ds[r] = du * slope;
-                ps[r] = p * slope;
+                ds[r] = CAP ? du * slope[r] : du;
+                ps[r] = CAP ? p * slope[r] : p;
             }
 #pragma unroll
             for (int k2 = 0; k2 < 2; ++k2) {
@@ -207,12 +228,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
 // 32) + r % 4) to sums by distance: lane L takes the entries whose key - query is L
 // or L - 32 from the lanes that hold them.  line[0] is the distance of key 0
 // and query 0 of the tile.
-__device__ __forceinline__ void add_diagonals(const float* du, float* line, int lr, int lh) {
+__device__ __forceinline__ void add_diagonals(const f32x16& du, float* line, int lr, int lh) {
     float pos = 0.f, neg = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int q = 8 * (r >> 2) + (r & 3) + 4 * lh, src = ((lr + q) & 31) + 32 * lh;
-        const float v = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * src, __builtin_bit_cast(int, du[r])));
+        const float mine = du[r];  // (a bit cast of the element itself reads element 0)
+        const float v = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(4 * src, __builtin_bit_cast(int, mine)));
         const bool wrap = lr + q >= 32;
         pos += wrap ? 0.f : v;
         neg += wrap ? v : 0.f;
@@ -224,8 +246,8 @@ __device__ __forceinline__ void add_diagonals(const float* du, float* line, int 
 
 // dk, dv and the bias gradient by distance.  WN waves take 32 keys each, 4 / WN
 // different queries of a tile.  Scores come as S = Q K^T here, keys on the lanes.
-template <class T, int DP, int WN, bool CAP>
-__global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn_dkv_kernel(AttnArgs x, BwdShape f) {
+template <class T, int DP, int WN, bool CAP, bool EXTRA>
+__global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnArgs x, BwdShape f) {
     constexpr int WK = 4 / WN, QB = bwd_kb(WN), QT = QB / 32 / WK, NK = DP / 16, ND = DP / 32;
     using TL = Tile<T, DP>;
     constexpr int TILE = QB * TL::LD, JW = 2 * DP * 32;
@@ -245,7 +267,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
     id /= a.kv_heads;
     const int b = id % a.batch, kt = id / a.batch, j0 = kt * 32 * WN;
     const Span s = span_of(a, b);
-    if (j0 >= s.nk) return;
+    if (j0 >= s.nk) {  // no such keys: their sums are zero
+        if (EXTRA && a.table)
+            for (int e = tid; e < G * (2 * R + 1); e += 256)
+                x.hist[(((int64_t)kt * a.batch + b) * a.heads + hk * G) * (2 * R + 1) + e] = 0.f;
+        return;
+    }
     const int pre = a.mask == FO_ATTN_PREFIX ? a.prefix[b] : 0, off = s.nk - s.nq;
     const int jw = j0 + 32 * wn, j = jw + lr;
     const bool ok = j < s.nk;
@@ -268,7 +295,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
         }
     }
     const ScoreK sc = score_k(a);
-    const bool bias = a.table != nullptr;
+    const bool bias = EXTRA && a.table != nullptr;
     const int W = lut_floats(a);
     float *lut = dyn, *line = dyn + (1 + w) * W;
     f32x16 dK[ND], dV[ND];
@@ -322,73 +349,79 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
                     Gd = mma(TL::frag_row(Gs, qw, 16 * kk, lane), v[kk], Gd);
                 }
                 const int n0 = jw - it - off;  // distance of key 0 and query 0 of the tile
-                const bool near = bias && n0 - 31 < R && n0 + 31 > -R;
-                const bool high = n0 - 31 >= R;
-                const float add0 = !bias ? 0.f : high ? far_hi : far_lo;
-                const int base = n0 + lr - 4 * lh + R + kReach;
-                const bool masked = it < wave_all;
-                const int from = first - it - 4 * lh;
-                uint2 keep[4];
-                const int kr = ((lr >> 3) << 2) | (lr & 3);  // the key's bit in a query's word
-                if (x.thr) {
-                    const uint32_t bits = keep_bits(x.thr, jw, lh, it + lr, b * a.heads + h, a);
-                    drops[w][32 * lh + lr] = (uint16_t)bits;
-                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4)
-                        keep[q4] = *reinterpret_cast<const uint2*>(&drops[w][32 * ((lr >> 2) & 1) + 8 * q4 + 4 * lh]);
-                    __builtin_amdgcn_wave_barrier();  // read before the next tile's words are written
+                const bool near = EXTRA && bias && n0 - 31 < R && n0 + 31 > -R, high = n0 - 31 >= R;
+                const float add0 = !bias || near ? 0.f : high ? far_hi : far_lo;
+                float slope[16];
+                to_exponent<T, CAP>(S, slope, sc, add0);
+                if (near) {
+                    const float* at = &lut[n0 + lr - 4 * lh + R + kReach];
+                    near_bias(S, [&](int r) { return at[-8 * (r >> 2) - (r & 3)]; });
                 }
-                float ds[16], ps[16];
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) {
                     const f32x4 ls = *reinterpret_cast<const f32x4*>(&sl[qw + 8 * q4 + 4 * lh]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[4 * q4 + e] -= ls[e];
+                }
+                if (it < wave_all) {
+                    const int from = first - it - 4 * lh;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r >> 2) + (r & 3) < from) S[r] = -INFINITY;
+                }
+                float ps[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ps[r] = S[r] = __builtin_amdgcn_exp2f(S[r]);
+                if (EXTRA && x.thr) {
+                    // drawn with the queries on the lanes, as in the other passes, and turned through LDS
+                    drops[w][32 * lh + lr] = (uint16_t)keep_bits(x.thr, jw, lh, it + lr, b * a.heads + h, a);
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                    const int kr = ((lr >> 3) << 2) | (lr & 3);  // the key's bit in a query's word
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        const uint2 words = *reinterpret_cast<const uint2*>(&drops[w][32 * ((lr >> 2) & 1) + 8 * q4 + 4 * lh]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool kept = ((e < 2 ? words.x : words.y) >> (kr + 16 * (e & 1))) & 1;
+                            Gd[4 * q4 + e] = kept ? Gd[4 * q4 + e] * x.keep_scale : 0.f;
+                            ps[4 * q4 + e] = kept ? ps[4 * q4 + e] : 0.f;
+                        }
+                    }
+                    __builtin_amdgcn_wave_barrier();  // read before the next tile's words are written
+                }
+#pragma unroll
+                for (int k2 = 0; k2 < 2; ++k2) {
+                    const Frag<T> pf = pack8<T>(ps + 8 * k2);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) dV[d] = mma(TL::frag_col(Gs, qw + 16 * k2, 32 * d, lane), pf, dV[d]);
+                }
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
                     const f32x4 dl = *reinterpret_cast<const f32x4*>(&sd[qw + 8 * q4 + 4 * lh]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * q4 + e, i = 8 * q4 + e;
-                        float slope = 1.f;
-                        const float add = near ? lut[base - i] : add0;
-                        const float u = CAP ? capped<T>(S[r], sc, &slope) + add : fmaf(S[r], sc.mul, add);
-                        float p = __builtin_amdgcn_exp2f(u - ls[e]);
-                        if (masked) p = i >= from ? p : 0.f;
-                        float dp = Gd[r];
-                        ps[r] = p;
-                        if (x.thr) {
-                            const uint32_t word = e < 2 ? keep[q4].x : keep[q4].y;
-                            const bool kept = (word >> (kr + 16 * (e & 1))) & 1;
-                            dp = kept ? dp * x.keep_scale : 0.f;
-                            ps[r] = kept ? p : 0.f;
-                        }
-                        const float du = p * (dp - dl[e]);
-                        Gd[r] = du;
-                        ds[r] = du * slope;
-                    }
+                    for (int e = 0; e < 4; ++e) S[4 * q4 + e] *= Gd[4 * q4 + e] - dl[e];  // dU
                 }
-                if (bias) {
-                    float du[16];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) du[r] = Gd[r];
+                if (EXTRA && bias) {
                     if (near) {
-                        add_diagonals(du, &line[n0 + R + kReach], lr, lh);
+                        add_diagonals(S, &line[n0 + R + kReach], lr, lh);
                     } else {
                         float sum = 0.f;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) sum += du[r];
+                        for (int r = 0; r < 16; ++r) sum += S[r];
                         if (high) sum_hi += sum;
                         else sum_lo += sum;
                     }
                 }
 #pragma unroll
                 for (int k2 = 0; k2 < 2; ++k2) {
-                    const Frag<T> df = pack8<T>(ds + 8 * k2), pf = pack8<T>(ps + 8 * k2);
+                    float ds[8];
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        dV[d] = mma(TL::frag_col(Gs, qw + 16 * k2, 32 * d, lane), pf, dV[d]);
-                        dK[d] = mma(TL::frag_col(Qs, qw + 16 * k2, 32 * d, lane), df, dK[d]);
-                    }
+                    for (int e = 0; e < 8; ++e) ds[e] = CAP ? S[8 * k2 + e] * slope[8 * k2 + e] : S[8 * k2 + e];
+                    const Frag<T> df = pack8<T>(ds);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) dK[d] = mma(TL::frag_col(Qs, qw + 16 * k2, 32 * d, lane), df, dK[d]);
                 }
             }
         }
@@ -448,28 +481,41 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 || DP == 128 ? 1 : 2) attn
 template <class T, int DP>
 fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
     const fo_attn& a = x.a;
-    const bool cap = a.cap > 0.f;
+    const bool cap = a.cap > 0.f, extra = a.table || x.thr;  // EXTRA: a bias or dropout
     const unsigned lds = a.table ? 4 * lut_floats(a) : 0;
     if (f.q_tiles) {
         const unsigned n = (unsigned)((int64_t)f.q_tiles * a.heads * a.batch);
-#define FO_DQ(W)                                                              \
-    if (cap) attn_dq_kernel<T, DP, W, true><<<n, 256, lds, s>>>(x, f);        \
-    else attn_dq_kernel<T, DP, W, false><<<n, 256, lds, s>>>(x, f)
-        if (f.wq == 1) { FO_DQ(1); }
-        else if (f.wq == 2) { FO_DQ(2); }
-        else { FO_DQ(4); }
+#define FO_DQ(W, CAP, EXTRA) attn_dq_kernel<T, DP, W, CAP, EXTRA><<<n, 256, lds, s>>>(x, f)
+#define FO_DQ_W(CAP, EXTRA)                              \
+    {                                                    \
+        if (f.wq == 1) FO_DQ(1, CAP, EXTRA);             \
+        else if (f.wq == 2) FO_DQ(2, CAP, EXTRA);        \
+        else FO_DQ(4, CAP, EXTRA);                       \
+    }
+        if (extra) {
+            if (cap) FO_DQ_W(true, true) else FO_DQ_W(false, true)
+        } else {
+            if (cap) FO_DQ_W(true, false) else FO_DQ_W(false, false)
+        }
+#undef FO_DQ_W
 #undef FO_DQ
         FO_LAUNCHED();
     }
     if (f.k_tiles) {
         const unsigned n = (unsigned)((int64_t)f.k_tiles * a.kv_heads * a.batch);
-#define FO_DKV(W)                                                             \
-    if (cap) attn_dkv_kernel<T, DP, W, true><<<n, 256, 5 * lds, s>>>(x, f);   \
-    else attn_dkv_kernel<T, DP, W, false><<<n, 256, 5 * lds, s>>>(x, f)
-        if constexpr (min_wk<T, DP>() == 1)
-            if (f.wk == 1) { FO_DKV(1); }
-        if (f.wk == 2) { FO_DKV(2); }
-        else if (f.wk == 4) { FO_DKV(4); }
+#define FO_DKV(W, CAP, EXTRA) attn_dkv_kernel<T, DP, W, CAP, EXTRA><<<n, 256, 5 * lds, s>>>(x, f)
+#define FO_DKV_W(CAP, EXTRA)                                         \
+    {                                                                \
+        if (f.wk == 4) FO_DKV(4, CAP, EXTRA);                        \
+        else if (f.wk == 2) FO_DKV(2, CAP, EXTRA);                   \
+        else if constexpr (min_wk<T, DP>() == 1) FO_DKV(1, CAP, EXTRA); \
+    }
+        if (extra) {
+            if (cap) FO_DKV_W(true, true) else FO_DKV_W(false, true)
+        } else {
+            if (cap) FO_DKV_W(true, false) else FO_DKV_W(false, false)
+        }
+#undef FO_DKV_W
 #undef FO_DKV
         FO_LAUNCHED();
     }

@@ -17,27 +17,32 @@ FO_EXTERN(float, 32); FO_EXTERN(float, 64); FO_EXTERN(float, 128);
 namespace {
 
 // The table's gradient from the key kernel's sums by distance: a workgroup per
-// head adds the tiles of every sequence in order, then each bucket's distances.
+// head, 256 distances at a time and four groups of threads on the tiles of all
+// sequences, which meet in order; then 32 threads per bucket.
 template <class T>
-__global__ void __launch_bounds__(256) bucket_sums(AttnArgs x, BwdShape f) {
+__global__ void __launch_bounds__(1024) bucket_sums(AttnArgs x, int parts) {
     const fo_attn& a = x.a;
-    __shared__ float sum[2 * 1024 + 1];
+    __shared__ float sum[4][2 * 1024 + 1];
     __shared__ int of[2 * 1024 + 1];
-    const int h = blockIdx.x, W = 2 * a.radius + 1;
-    for (int n = threadIdx.x; n < W; n += 256) {
+    const int h = blockIdx.x, W = 2 * a.radius + 1, tid = threadIdx.x, g4 = tid >> 8;
+    const float* hist = x.hist + (int64_t)h * W;
+    const int64_t step = (int64_t)a.heads * W;
+    for (int n = tid & 255; n < W; n += 256) {
         float s = 0.f;
-        for (int b = 0; b < a.batch; ++b) {
-            const int tiles = (span_of(a, b).nk + 32 * f.wk - 1) / (32 * f.wk);
-            for (int t = 0; t < tiles; ++t) s += x.hist[(((int64_t)t * a.batch + b) * a.heads + h) * W + n];
-        }
-        sum[n] = s;
-        of[n] = min(max(a.bucket[n], 0), a.n_buckets - 1);
+#pragma unroll 8
+        for (int p = g4; p < parts; p += 4) s += hist[p * step + n];
+        sum[g4][n] = s;
+        if (g4 == 0) of[n] = min(max(a.bucket[n], 0), a.n_buckets - 1);
     }
     __syncthreads();
-    for (int g = threadIdx.x; g < a.n_buckets; g += 256) {
+    for (int n = tid; n < W; n += 1024) sum[0][n] = sum[0][n] + sum[1][n] + sum[2][n] + sum[3][n];
+    __syncthreads();
+    for (int g = tid >> 5; g < a.n_buckets; g += 32) {
         float s = 0.f;
-        for (int n = 0; n < W; ++n) s += of[n] == g ? sum[n] : 0.f;
-        ((T*)x.dtable)[(int64_t)g * a.heads + h] = from_f<T>(s);
+        for (int n = tid & 31; n < W; n += 32) s += of[n] == g ? sum[0][n] : 0.f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor(s, o);
+        if ((tid & 31) == 0) ((T*)x.dtable)[(int64_t)g * a.heads + h] = from_f<T>(s);
     }
 }
 
@@ -155,7 +160,7 @@ static fo_status bwd(const AttnArgs& x, hipStream_t s) {
                          : a.head_dim <= 64 ? attn_bwd_launch<T, 64>(x, f, s)
                                             : attn_bwd_launch<T, 128>(x, f, s);
     if (st != FO_OK || !a.table) return st;
-    bucket_sums<T><<<(unsigned)a.heads, 256, 0, s>>>(x, f);
+    bucket_sums<T><<<(unsigned)a.heads, 1024, 0, s>>>(x, f.k_tiles * a.batch);
     FO_LAUNCHED();
     return FO_OK;
 }
