@@ -17,7 +17,9 @@ namespace fo {
 struct BwdShape {
     int wq, q_tiles;  // query kernel: waves side by side over rows, row tiles
     int wk, k_tiles;  // key kernel: the same over keys
+    int h_parts, q_parts;  // and its cuts over a key head's heads and over the queries
     bool vec;
+    float* part;  // partial dk, then dv, of the cuts: [h_parts q_parts][k_rows][kv_heads][D] each
 };
 
 // The key kernel's waves side by side, at least: with fp32 rows of 128, four
@@ -246,6 +248,8 @@ __device__ __forceinline__ void add_diagonals(const f32x16& du, float* line, int
 
 // dk, dv and the bias gradient by distance.  WN waves take 32 keys each, 4 / WN
 // different queries of a tile.  Scores come as S = Q K^T here, keys on the lanes.
+// Where there are few key tiles the work of one is cut over the heads that share
+// it and over the queries, and join_keys adds the cuts.
 template <class T, int DP, int WN, bool CAP, bool EXTRA>
 __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnArgs x, BwdShape f) {
     constexpr int WK = 4 / WN, QB = bwd_kb(WN), QT = QB / 32 / WK, NK = DP / 16, ND = DP / 32;
@@ -265,12 +269,18 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
     int id = blockIdx.x;
     const int hk = id % a.kv_heads;
     id /= a.kv_heads;
-    const int b = id % a.batch, kt = id / a.batch, j0 = kt * 32 * WN;
+    const int b = id % a.batch;
+    id /= a.batch;
+    const int parts = f.h_parts * f.q_parts, part = id % parts, qp = part / f.h_parts, kt = id / parts;
+    const int j0 = kt * 32 * WN, hb = (G + f.h_parts - 1) / f.h_parts;
+    const int h0 = min(part % f.h_parts * hb, G), h1 = min(h0 + hb, G);  // the workgroup's heads of the group
+    float* hist = EXTRA && a.table
+                      ? x.hist + ((((int64_t)qp * f.k_tiles + kt) * a.batch + b) * a.heads + hk * G) * (2 * R + 1)
+                      : nullptr;
     const Span s = span_of(a, b);
     if (j0 >= s.nk) {  // no such keys: their sums are zero
-        if (EXTRA && a.table)
-            for (int e = tid; e < G * (2 * R + 1); e += 256)
-                x.hist[(((int64_t)kt * a.batch + b) * a.heads + hk * G) * (2 * R + 1) + e] = 0.f;
+        if (hist)
+            for (int e = h0 * (2 * R + 1) + tid; e < h1 * (2 * R + 1); e += 256) hist[e] = 0.f;
         return;
     }
     const int pre = a.mask == FO_ATTN_PREFIX ? a.prefix[b] : 0, off = s.nk - s.nq;
@@ -281,7 +291,12 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
     const int first = ok ? first_of(j) : 0x7fffffff;
     const int wave_from = jw < s.nk ? first_of(jw) : 0x7fffffff;
     const int wave_all = jw + 32 <= s.nk ? first_of(jw + 31) : 0x7fffffff;  // all 32 keys are seen from here on
-    const int t0 = min(first_of(j0), s.nq) / QB, t1 = (s.nq + QB - 1) / QB;
+    int t0 = min(first_of(j0), s.nq) / QB, t1 = (s.nq + QB - 1) / QB;
+    {
+        const int per = (t1 - t0 + f.q_parts - 1) / f.q_parts;
+        t0 = min(t0 + qp * per, t1);
+        t1 = min(t0 + per, t1);
+    }
 
     Frag<T> k[NK], v[NK];
     {
@@ -304,7 +319,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
 #pragma unroll
         for (int r = 0; r < 16; ++r) dK[d][r] = dV[d][r] = 0.f;
 
-    for (int h = hk * G; h < hk * G + G; ++h) {
+    for (int hg = h0; hg < h1; ++hg) {
+        const int h = hk * G + hg;
         const T* qb = (const T*)x.q + (int64_t)s.q0 * a.q_ld + h * a.q_hs;
         const T* gb = (const T*)x.dout + (int64_t)s.q0 * a.out_ld + h * a.out_hs;
         const int64_t stat = (int64_t)h * a.q_rows + s.q0;
@@ -436,14 +452,16 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
                 line[W - 1] += sum_hi;
             }
             __syncthreads();
-            float* out = x.hist + (((int64_t)kt * a.batch + b) * a.heads + h) * (2 * R + 1);
-            for (int n = tid; n < 2 * R + 1; n += 256) {
-                const int lo = n == 0 ? 0 : n + kReach, hi = n == 2 * R ? W - 1 : n + kReach;
+            float* out = hist + hg * (2 * R + 1);
+            auto all = [&](int e) { return dyn[W + e] + dyn[2 * W + e] + dyn[3 * W + e] + dyn[4 * W + e]; };
+            if (w < (R ? 2 : 1)) {  // a wave for each end; without a radius all distances are one
                 float sum = 0.f;
-                for (int e = lo; e <= hi; ++e)
-                    for (int y = 0; y < 4; ++y) sum += dyn[(1 + y) * W + e];
-                out[n] = sum;
+                for (int e = lane; e < (R ? kReach + 1 : W); e += 64) sum += all(w ? W - 1 - e : e);
+#pragma unroll
+                for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+                if (lane == 0) out[w * 2 * R] = sum;
             }
+            for (int n = 1 + tid; n < 2 * R; n += 256) out[n] = all(n + kReach);
         }
     }
     if (WK > 1) {
@@ -474,6 +492,13 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
         }
     }
     if (!ok) return;
+    if (parts > 1) {
+        const int64_t at = (((int64_t)part * a.k_rows + s.k0 + j) * a.kv_heads + hk) * D;
+        const int64_t all = (int64_t)parts * a.k_rows * a.kv_heads * D;
+        store_row<float, DP>(f.part + at, dK, 1.f, lh, D, (D & 3) == 0);
+        store_row<float, DP>(f.part + all + at, dV, 1.f, lh, D, (D & 3) == 0);
+        return;
+    }
     store_row<T, DP>((T*)x.dk + (int64_t)(s.k0 + j) * a.k_ld + hk * a.k_hs, dK, a.scale, lh, D, f.vec);
     store_row<T, DP>((T*)x.dv + (int64_t)(s.k0 + j) * a.v_ld + hk * a.v_hs, dV, x.keep_scale, lh, D, f.vec);
 }
@@ -502,7 +527,7 @@ fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
         FO_LAUNCHED();
     }
     if (f.k_tiles) {
-        const unsigned n = (unsigned)((int64_t)f.k_tiles * a.kv_heads * a.batch);
+        const unsigned n = (unsigned)((int64_t)f.k_tiles * f.h_parts * f.q_parts * a.kv_heads * a.batch);
 #define FO_DKV(W, CAP, EXTRA) attn_dkv_kernel<T, DP, W, CAP, EXTRA><<<n, 256, 5 * lds, s>>>(x, f)
 #define FO_DKV_W(CAP, EXTRA)                                         \
     {                                                                \

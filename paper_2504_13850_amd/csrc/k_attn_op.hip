@@ -79,6 +79,35 @@ __global__ void __launch_bounds__(256) join_slices(AttnArgs x, FwdShape f) {
     if (x.lse && lane == 0) x.lse[row] = l > 0.f ? m + __builtin_amdgcn_logf(l) : -INFINITY;
 }
 
+// Adds the key kernel's cuts of a key row in order: one wave per row and key head.
+template <class T>
+__global__ void __launch_bounds__(256) join_keys(AttnArgs x, BwdShape f) {
+    const fo_attn& a = x.a;
+    const int lane = threadIdx.x & 63, D = a.head_dim, parts = f.h_parts * f.q_parts;
+    int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int hk = (int)(id % a.kv_heads);
+    id /= a.kv_heads;
+    const int j = (int)(id % a.max_k), b = (int)(id / a.max_k);
+    if (b >= a.batch) return;
+    const Span s = span_of(a, b);
+    if (j >= s.nk) return;
+    const int64_t step = a.k_rows * a.kv_heads * D;
+    const float* dk = f.part + ((int64_t)(s.k0 + j) * a.kv_heads + hk) * D;
+    const float* dv = dk + parts * step;
+    T* outk = (T*)x.dk + (int64_t)(s.k0 + j) * a.k_ld + hk * a.k_hs;
+    T* outv = (T*)x.dv + (int64_t)(s.k0 + j) * a.v_ld + hk * a.v_hs;
+    for (int c = lane; c < D; c += 64) {
+        float sk = 0.f, sv = 0.f;
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            sk += dk[p * step + c];
+            sv += dv[p * step + c];
+        }
+        outk[c] = from_f<T>(sk * a.scale);
+        outv[c] = from_f<T>(sv * x.keep_scale);
+    }
+}
+
 // 16-byte aligned rows of a [rows][heads][dim] operand.
 bool aligned_rows(const void* p, int64_t ld, int64_t hs, int64_t size) {
     return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && hs * size % 16 == 0;
@@ -113,7 +142,21 @@ BwdShape bwd_shape(const fo_attn& a) {
     f.q_tiles = a.q_rows ? (int)cdiv(a.max_q, 32 * f.wq) : 0;
     f.wk = a.max_k > 64 ? 4 : a.max_k > 32 || (a.dtype == FO_DT_F32 && a.head_dim > 64) ? 2 : 1;  // see min_wk
     f.k_tiles = a.k_rows ? (int)cdiv(a.max_k, 32 * f.wk) : 0;
+    // The key kernel's work is cut until about 512 workgroups share it, each with
+    // 512 query rows of one head or more, so that the cuts' sums stay a small part.
+    const int64_t wgs = std::max<int64_t>(1, (int64_t)f.k_tiles * a.kv_heads * a.batch), G = a.heads / a.kv_heads;
+    const int64_t cuts = std::max<int64_t>(1, std::min<int64_t>({cdiv(512, wgs), G * a.max_q / 512, 64}));
+    f.h_parts = (int)std::min(G, cuts);
+    while (G % f.h_parts) --f.h_parts;
+    f.q_parts = (int)(cuts / f.h_parts);
     return f;
+}
+int64_t part_floats(const fo_attn& a, const BwdShape& f) {
+    const int64_t parts = (int64_t)f.h_parts * f.q_parts;
+    return parts > 1 ? (2 * parts * a.k_rows * a.kv_heads * a.head_dim + 3) & ~int64_t(3) : 0;
+}
+int64_t hist_floats(const fo_attn& a, const BwdShape& f) {
+    return a.table ? (int64_t)f.q_parts * f.k_tiles * a.batch * a.heads * (2 * a.radius + 1) : 0;
 }
 // delta of every row and head, in whole 16-byte units
 int64_t stat_floats(const fo_attn& a) { return (a.q_rows * a.heads + 3) & ~int64_t(3); }
@@ -125,8 +168,8 @@ int64_t attn_workspace(const fo_attn& a, bool backward) {
         const FwdShape f = fwd_shape(a);
         return f.splits > 1 ? (int64_t)f.splits * a.heads * a.q_rows * (a.head_dim + 2) * 4 : 0;
     }
-    return stat_floats(a) * 4 +
-           (a.table ? (int64_t)bwd_shape(a).k_tiles * a.batch * a.heads * (2 * a.radius + 1) * 4 : 0);
+    const BwdShape f = bwd_shape(a);
+    return 4 * (stat_floats(a) + part_floats(a, f) + hist_floats(a, f));
 }
 
 template <class T>
@@ -150,25 +193,32 @@ fo_status launch_attn_op_fwd(const AttnArgs& x, void* ws, hipStream_t s) {
 }
 
 template <class T>
-static fo_status bwd(const AttnArgs& x, hipStream_t s) {
+static fo_status bwd(AttnArgs& x, float* ws, hipStream_t s) {
     const fo_attn& a = x.a;
     const int64_t e = sizeof(T);
     BwdShape f = bwd_shape(a);
+    x.delta = ws;
+    f.part = ws + stat_floats(a);
+    x.hist = f.part + part_floats(a, f);
     f.vec = vec_fwd(x) && aligned_rows(x.dout, a.out_ld, a.out_hs, e) && aligned_rows(x.dq, a.q_ld, a.q_hs, e) &&
             aligned_rows(x.dk, a.k_ld, a.k_hs, e) && aligned_rows(x.dv, a.v_ld, a.v_hs, e);
     const fo_status st = a.head_dim <= 32   ? attn_bwd_launch<T, 32>(x, f, s)
                          : a.head_dim <= 64 ? attn_bwd_launch<T, 64>(x, f, s)
                                             : attn_bwd_launch<T, 128>(x, f, s);
-    if (st != FO_OK || !a.table) return st;
-    bucket_sums<T><<<(unsigned)a.heads, 1024, 0, s>>>(x, f.k_tiles * a.batch);
-    FO_LAUNCHED();
+    if (st != FO_OK) return st;
+    if (part_floats(a, f)) {
+        join_keys<T><<<(unsigned)cdiv((int64_t)a.batch * a.max_k * a.kv_heads, 4), 256, 0, s>>>(x, f);
+        FO_LAUNCHED();
+    }
+    if (a.table) {
+        bucket_sums<T><<<(unsigned)a.heads, 1024, 0, s>>>(x, f.q_parts * f.k_tiles * a.batch);
+        FO_LAUNCHED();
+    }
     return FO_OK;
 }
 
 fo_status launch_attn_op_bwd(AttnArgs& x, void* ws, hipStream_t s) {
-    x.delta = (float*)ws;
-    x.hist = x.delta + stat_floats(x.a);
-    return x.a.dtype == FO_DT_BF16 ? bwd<bf16_t>(x, s) : bwd<float>(x, s);
+    return x.a.dtype == FO_DT_BF16 ? bwd<bf16_t>(x, (float*)ws, s) : bwd<float>(x, (float*)ws, s);
 }
 
 }  // namespace fo
