@@ -51,7 +51,7 @@ __device__ __forceinline__ void near_bias(f32x16& S, F f) {
 // kernel also sums X_i = sum_j P_ij du/ds k_j and subtracts e_i X_i: one more
 // product instead of a pass for delta, which would take two and the
 // exponentials again.
-template <class T, int DP, int WQ, bool CAP, bool EXTRA>
+template <class T, int DP, int WQ, bool CAP, bool EXTRA, bool VEC>
 __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnArgs x, BwdShape f) {
     constexpr int WK = 4 / WQ, KB = bwd_kb(WQ), KT = KB / 32 / WK, NK = DP / 16, ND = DP / 32;
     constexpr bool FIX = sizeof(T) == 2;
@@ -83,10 +83,10 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
 
     const T* kb = (const T*)x.k + (int64_t)s.k0 * a.k_ld + hk * a.k_hs;
     const T* vb = (const T*)x.v + (int64_t)s.k0 * a.v_ld + hk * a.v_hs;
-    Stage<T, DP, KB> sk, sv;
+    Stage<T, DP, KB, VEC> sk, sv;
     if (tiles) {
-        sk.load(kb, a.k_ld, 0, s.nk, D, f.vec, tid);
-        sv.load(vb, a.v_ld, 0, s.nk, D, f.vec, tid);
+        sk.load(kb, a.k_ld, 0, s.nk, D, tid);
+        sv.load(vb, a.v_ld, 0, s.nk, D, tid);
     }
     const int64_t stat = (int64_t)h * a.q_rows + s.q0 + qi;
     Frag<T> q[NK], g[NK];
@@ -98,11 +98,12 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
         const T* orow = (const T*)x.out + row * a.out_ld + h * a.out_hs;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            q[kk] = ld_frag(qr, 16 * kk + 8 * lh, D, ok, f.vec);
-            g[kk] = ld_frag(gr, 16 * kk + 8 * lh, D, ok, f.vec);
-            const Frag<T> o = ld_frag(orow, 16 * kk + 8 * lh, D, ok, f.vec);
+            q[kk] = ld_frag<VEC>(qr, 16 * kk + 8 * lh, D, ok);
+            g[kk] = ld_frag<VEC>(gr, 16 * kk + 8 * lh, D, ok);
+            const Frag<T> o = ld_frag<VEC>(orow, 16 * kk + 8 * lh, D, ok);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dl = fmaf((float)g[kk].v[e], (float)o.v[e], dl);
+            if (!CAP && a.scale < 0.f) negate(q[kk]);
         }
         dl += __shfl_xor(dl, 32);
     }
@@ -129,8 +130,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
         sv.store(Vs, tid);
         __syncthreads();
         if (t + 1 < tiles) {
-            sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, f.vec, tid);
-            sv.load(vb, a.v_ld, (t + 1) * KB, s.nk, D, f.vec, tid);
+            sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, tid);
+            sv.load(vb, a.v_ld, (t + 1) * KB, s.nk, D, tid);
         }
 #pragma unroll
         for (int c = 0; c < KT; ++c) {
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
             for (int r = 0; r < 16; ++r) dQ[d][r] = fmaf(-err, X[d][r], dQ[d][r]);
         dl += err;
     }
-    store_row<T, DP>((T*)x.dq + (int64_t)(s.q0 + qi) * a.q_ld + h * a.q_hs, dQ, a.scale, lh, D, f.vec);
+    store_row<T, DP>((T*)x.dq + (int64_t)(s.q0 + qi) * a.q_ld + h * a.q_hs, dQ, a.scale, lh, D, VEC);
     if (lh == 0) x.delta[stat] = dl;
 }
 
@@ -250,7 +251,7 @@ __device__ __forceinline__ void add_diagonals(const f32x16& du, float* line, int
 // different queries of a tile.  Scores come as S = Q K^T here, keys on the lanes.
 // Where there are few key tiles the work of one is cut over the heads that share
 // it and over the queries, and join_keys adds the cuts.
-template <class T, int DP, int WN, bool CAP, bool EXTRA>
+template <class T, int DP, int WN, bool CAP, bool EXTRA, bool VEC>
 __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnArgs x, BwdShape f) {
     constexpr int WK = 4 / WN, QB = bwd_kb(WN), QT = QB / 32 / WK, NK = DP / 16, ND = DP / 32;
     using TL = Tile<T, DP>;
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
     const Span s = span_of(a, b);
     if (j0 >= s.nk) {  // no such keys: their sums are zero
         if (hist)
-            for (int e = h0 * (2 * R + 1) + tid; e < h1 * (2 * R + 1); e += 256) hist[e] = 0.f;
+            each(tid, 256, (h1 - h0) * (2 * R + 1), [&](int e) { hist[h0 * (2 * R + 1) + e] = 0.f; });
         return;
     }
     const int pre = a.mask == FO_ATTN_PREFIX ? a.prefix[b] : 0, off = s.nk - s.nq;
@@ -305,8 +306,9 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
         const T* vr = (const T*)x.v + row * a.v_ld + hk * a.v_hs;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk) {
-            k[kk] = ld_frag(kr, 16 * kk + 8 * lh, D, ok, f.vec);
-            v[kk] = ld_frag(vr, 16 * kk + 8 * lh, D, ok, f.vec);
+            k[kk] = ld_frag<VEC>(kr, 16 * kk + 8 * lh, D, ok);
+            v[kk] = ld_frag<VEC>(vr, 16 * kk + 8 * lh, D, ok);
+            if (!CAP && a.scale < 0.f) negate(k[kk]);
         }
     }
     const ScoreK sc = score_k(a);
@@ -330,13 +332,13 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
             far_lo = bias_at<T>(a, h, -R);
             far_hi = bias_at<T>(a, h, R);
             fill_lut<T>(lut, a, h, tid);
-            for (int n = lane; n < W; n += 64) line[n] = 0.f;
+            each(lane, 64, W, [&](int n) { line[n] = 0.f; });
         }
-        Stage<T, DP, QB> sq, sg;
+        Stage<T, DP, QB, VEC> sq, sg;
         float pl = 0.f, pd = 0.f;
         auto load = [&](int t) {
-            sq.load(qb, a.q_ld, t * QB, s.nq, D, f.vec, tid);
-            sg.load(gb, a.out_ld, t * QB, s.nq, D, f.vec, tid);
+            sq.load(qb, a.q_ld, t * QB, s.nq, D, tid);
+            sg.load(gb, a.out_ld, t * QB, s.nq, D, tid);
             if (tid < QB) {
                 const int i = t * QB + tid;
                 pl = i < s.nq ? x.lse[stat + i] : INFINITY;  // no such row: P = exp2(-inf) = 0
@@ -456,12 +458,12 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
             auto all = [&](int e) { return dyn[W + e] + dyn[2 * W + e] + dyn[3 * W + e] + dyn[4 * W + e]; };
             if (w < (R ? 2 : 1)) {  // a wave for each end; without a radius all distances are one
                 float sum = 0.f;
-                for (int e = lane; e < (R ? kReach + 1 : W); e += 64) sum += all(w ? W - 1 - e : e);
+                each(lane, 64, R ? kReach + 1 : W, [&](int e) { sum += all(w ? W - 1 - e : e); });
 #pragma unroll
                 for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
                 if (lane == 0) out[w * 2 * R] = sum;
             }
-            for (int n = 1 + tid; n < 2 * R; n += 256) out[n] = all(n + kReach);
+            each(tid, 256, 2 * R - 1, [&](int n) { out[1 + n] = all(1 + n + kReach); });
         }
     }
     if (WK > 1) {
@@ -499,8 +501,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
         store_row<float, DP>(f.part + all + at, dV, 1.f, lh, D, (D & 3) == 0);
         return;
     }
-    store_row<T, DP>((T*)x.dk + (int64_t)(s.k0 + j) * a.k_ld + hk * a.k_hs, dK, a.scale, lh, D, f.vec);
-    store_row<T, DP>((T*)x.dv + (int64_t)(s.k0 + j) * a.v_ld + hk * a.v_hs, dV, x.keep_scale, lh, D, f.vec);
+    store_row<T, DP>((T*)x.dk + (int64_t)(s.k0 + j) * a.k_ld + hk * a.k_hs, dK, a.scale, lh, D, VEC);
+    store_row<T, DP>((T*)x.dv + (int64_t)(s.k0 + j) * a.v_ld + hk * a.v_hs, dV, x.keep_scale, lh, D, VEC);
 }
 
 template <class T, int DP>
@@ -510,12 +512,13 @@ fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
     const unsigned lds = a.table ? 4 * lut_floats(a) : 0;
     if (f.q_tiles) {
         const unsigned n = (unsigned)((int64_t)f.q_tiles * a.heads * a.batch);
-#define FO_DQ(W, CAP, EXTRA) attn_dq_kernel<T, DP, W, CAP, EXTRA><<<n, 256, lds, s>>>(x, f)
-#define FO_DQ_W(CAP, EXTRA)                              \
-    {                                                    \
-        if (f.wq == 1) FO_DQ(1, CAP, EXTRA);             \
-        else if (f.wq == 2) FO_DQ(2, CAP, EXTRA);        \
-        else FO_DQ(4, CAP, EXTRA);                       \
+#define FO_DQ(W, CAP, EXTRA, VEC) attn_dq_kernel<T, DP, W, CAP, EXTRA, VEC><<<n, 256, lds, s>>>(x, f)
+#define FO_DQ_W(CAP, EXTRA)                                    \
+    {                                                          \
+        if (!f.vec) FO_DQ(4, CAP, EXTRA, false);               \
+        else if (f.wq == 1) FO_DQ(1, CAP, EXTRA, true);        \
+        else if (f.wq == 2) FO_DQ(2, CAP, EXTRA, true);        \
+        else FO_DQ(4, CAP, EXTRA, true);                       \
     }
         if (extra) {
             if (cap) FO_DQ_W(true, true) else FO_DQ_W(false, true)
@@ -528,12 +531,13 @@ fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
     }
     if (f.k_tiles) {
         const unsigned n = (unsigned)((int64_t)f.k_tiles * f.h_parts * f.q_parts * a.kv_heads * a.batch);
-#define FO_DKV(W, CAP, EXTRA) attn_dkv_kernel<T, DP, W, CAP, EXTRA><<<n, 256, 5 * lds, s>>>(x, f)
-#define FO_DKV_W(CAP, EXTRA)                                         \
-    {                                                                \
-        if (f.wk == 4) FO_DKV(4, CAP, EXTRA);                        \
-        else if (f.wk == 2) FO_DKV(2, CAP, EXTRA);                   \
-        else if constexpr (min_wk<T, DP>() == 1) FO_DKV(1, CAP, EXTRA); \
+#define FO_DKV(W, CAP, EXTRA, VEC) attn_dkv_kernel<T, DP, W, CAP, EXTRA, VEC><<<n, 256, 5 * lds, s>>>(x, f)
+#define FO_DKV_W(CAP, EXTRA)                                                  \
+    {                                                                         \
+        if (!f.vec) FO_DKV(4, CAP, EXTRA, false);                             \
+        else if (f.wk == 4) FO_DKV(4, CAP, EXTRA, true);                      \
+        else if (f.wk == 2) FO_DKV(2, CAP, EXTRA, true);                      \
+        else if constexpr (min_wk<T, DP>() == 1) FO_DKV(1, CAP, EXTRA, true); \
     }
         if (extra) {
             if (cap) FO_DKV_W(true, true) else FO_DKV_W(false, true)

@@ -18,19 +18,20 @@ constexpr int fwd_kb(int wq) { return 32 * fwd_kt(wq) * (4 / wq); }
 
 // out = softmax(u) V with running maximum m and sum l.  Four waves: WQ of them
 // take 32 rows each, 4 / WQ take different keys of a tile and join at the end.
-// K and V tiles pass through registers into one LDS buffer, the next tile's
-// loads in flight during the products.
-template <class T, int DP, int WQ, bool CAP, bool DROP>
+// K and V tiles pass through registers into LDS, the next tile's loads in flight
+// during the products.  EXTRA: a bias or dropout.  VEC: see ld_chunk.
+template <class T, int DP, int WQ, bool CAP, bool EXTRA, bool VEC>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 && DP > 32 ? 1 : 2)
 attn_fwd_kernel(AttnArgs x, FwdShape f) {
     constexpr int WK = 4 / WQ, KT = fwd_kt(WQ), KB = fwd_kb(WQ), NK = DP / 16, ND = DP / 32;
     using TL = Tile<T, DP>;
     constexpr int TILE = KB * TL::LD;
     constexpr int JOIN = WK > 1 ? (WK - 1) * WQ * 32 * (DP + 2) : 0;  // floats
-    constexpr int BYTES = 2 * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * TILE * (int)sizeof(T) : JOIN * 4;
+    // a second buffer saves one of two barriers a tile, where two workgroups still fit
+    constexpr int BUF = WQ > 1 && 4 * TILE * (int)sizeof(T) <= 65536 ? 2 : 1;
+    constexpr int BYTES = 2 * BUF * TILE * (int)sizeof(T) > JOIN * 4 ? 2 * BUF * TILE * (int)sizeof(T) : JOIN * 4;
     __shared__ __attribute__((aligned(16))) char smem[BYTES];
     extern __shared__ float lut[];  // with a bias: its values by distance
-    T *Ks = (T*)smem, *Vs = Ks + TILE;
     const fo_attn& a = x.a;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 31, lh = lane >> 5;
     const int wq = w % WQ, wk = w / WQ;
@@ -63,19 +64,22 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
 
     const T* kb = (const T*)x.k + (int64_t)s.k0 * a.k_ld + hk * a.k_hs;
     const T* vb = (const T*)x.v + (int64_t)s.k0 * a.v_ld + hk * a.v_hs;
-    Stage<T, DP, KB> sk, sv;
+    Stage<T, DP, KB, VEC> sk, sv;
     if (t0 < t1) {
-        sk.load(kb, a.k_ld, t0 * KB, s.nk, D, f.vec, tid);
-        sv.load(vb, a.v_ld, t0 * KB, s.nk, D, f.vec, tid);
+        sk.load(kb, a.k_ld, t0 * KB, s.nk, D, tid);
+        sv.load(vb, a.v_ld, t0 * KB, s.nk, D, tid);
     }
     Frag<T> q[NK];
     {
         const T* row = (const T*)x.q + (int64_t)(s.q0 + (ok ? qi : 0)) * a.q_ld + (ok ? head : h0) * a.q_hs;
 #pragma unroll
-        for (int kk = 0; kk < NK; ++kk) q[kk] = ld_frag(row, 16 * kk + 8 * lh, D, ok, f.vec);
+        for (int kk = 0; kk < NK; ++kk) {
+            q[kk] = ld_frag<VEC>(row, 16 * kk + 8 * lh, D, ok);
+            if (!CAP && a.scale < 0.f) negate(q[kk]);
+        }
     }
     const ScoreK sc = score_k(a);
-    const bool bias = a.table != nullptr;
+    const bool bias = EXTRA && a.table != nullptr;
     float far_lo = 0.f, far_hi = 0.f;  // bias beyond the radius on either side
     if (bias) {
         far_lo = bias_at<T>(a, ok ? head : h0, -a.radius);
@@ -91,13 +95,14 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
     float m = -INFINITY, l = 0.f;  // l: this lane's keys only
 
     for (int t = t0; t < t1; ++t) {
-        __syncthreads();  // the previous tile has been read
+        T *Ks = (T*)smem + (BUF == 2 ? (t & 1) * 2 * TILE : 0), *Vs = Ks + TILE;
+        if (BUF == 1) __syncthreads();  // the previous tile has been read
         sk.store(Ks, tid);
         sv.store(Vs, tid);
         __syncthreads();
         if (t + 1 < t1) {
-            sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, f.vec, tid);
-            sv.load(vb, a.v_ld, (t + 1) * KB, s.nk, D, f.vec, tid);
+            sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, tid);
+            sv.load(vb, a.v_ld, (t + 1) * KB, s.nk, D, tid);
         }
         const int kw = 32 * KT * wk, j0 = t * KB + kw;  // the wave's first key in the tile, in the sequence
         if (j0 >= wave_end) continue;
@@ -111,10 +116,10 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
         }
         // distances of the wave's rows to this tile: [n_lo, n_hi]
         const int n_lo = j0 - (f.pack ? 0 : iw + 31) - off, n_hi = j0 + 32 * KT - 1 - (f.pack ? 0 : iw) - off;
-        const bool near = bias && n_lo < a.radius && n_hi > -a.radius;
-        const float add0 = !bias ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
+        const bool near = EXTRA && bias && n_lo < a.radius && n_hi > -a.radius;
+        const float add0 = !EXTRA || !bias ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
         float mul = sc.mul, add = add0;
-        if (CAP || near || sc.mul <= 0.f) {  // x itself takes S's place
+        if (CAP || near) {  // x itself takes S's place
             const int base = j0 + 4 * lh - qi - off;
 #pragma unroll
             for (int c = 0; c < KT; ++c)
@@ -149,6 +154,7 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
         // The maximum is moved up only when some row's grew by more than 2^8: the sums
         // stay far inside fp32, and most tiles leave the accumulators alone.
         if (__any(mn > m + 8.f)) {
+            asm volatile("");  // a branch, not 16 ND products every time
             const float g = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
             l *= g;
 #pragma unroll
@@ -166,7 +172,7 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
                 p[r] = __builtin_amdgcn_exp2f(fmaf(S[c][r], mul, sub));
                 l += p[r];
             }
-            if (DROP) {
+            if (EXTRA && x.thr) {
                 const uint32_t bits = keep_bits(x.thr, j0 + 32 * c, lh, qi, b * a.heads + head, a);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p[r] = (bits >> r) & 1 ? p[r] : 0.f;
@@ -217,7 +223,7 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
         return;
     }
     const float inv = l > 0.f ? x.keep_scale / l : 0.f;
-    store_row<T, DP>((T*)x.out + (int64_t)(s.q0 + qi) * a.out_ld + head * a.out_hs, O, inv, lh, D, f.vec);
+    store_row<T, DP>((T*)x.out + (int64_t)(s.q0 + qi) * a.out_ld + head * a.out_hs, O, inv, lh, D, VEC);
     if (x.lse && lh == 0)
         x.lse[(int64_t)head * a.q_rows + s.q0 + qi] = l > 0.f ? m + __builtin_amdgcn_logf(l) : -INFINITY;
 }
@@ -229,14 +235,20 @@ fo_status attn_fwd_launch(const AttnArgs& x, const FwdShape& f, hipStream_t s) {
     const int64_t n = (int64_t)f.row_tiles * (f.pack ? a.kv_heads : a.heads) * a.batch * f.splits;
     const bool cap = a.cap > 0.f;
     const unsigned lds = a.table && !f.pack ? 4 * lut_floats(a) : 0;
-#define FO_FWD(WQ, CAP, DROP) attn_fwd_kernel<T, DP, WQ, CAP, DROP><<<(unsigned)n, 256, lds, s>>>(x, f)
-#define FO_FWD_W(CAP, DROP)                              \
-    {                                                    \
-        if (f.wq == 1) FO_FWD(1, CAP, DROP);             \
-        else if (f.wq == 2) FO_FWD(2, CAP, DROP);        \
-        else FO_FWD(4, CAP, DROP);                       \
+    const bool extra = a.table || x.thr;
+#define FO_FWD(WQ, CAP, EXTRA, VEC) attn_fwd_kernel<T, DP, WQ, CAP, EXTRA, VEC><<<(unsigned)n, 256, lds, s>>>(x, f)
+#define FO_FWD_W(CAP, EXTRA)                                   \
+    {                                                          \
+        if (!f.vec) {  /* 33 to 64 rows: one tile either way */ \
+            if (f.wq == 1) FO_FWD(1, CAP, EXTRA, false);       \
+            else FO_FWD(4, CAP, EXTRA, false);                 \
+        } else {                                               \
+            if (f.wq == 1) FO_FWD(1, CAP, EXTRA, true);        \
+            else if (f.wq == 2) FO_FWD(2, CAP, EXTRA, true);   \
+            else FO_FWD(4, CAP, EXTRA, true);                  \
+        }                                                      \
     }
-    if (x.thr) {
+    if (extra) {
         if (cap) FO_FWD_W(true, true) else FO_FWD_W(false, true)
     } else {
         if (cap) FO_FWD_W(true, false) else FO_FWD_W(false, false)

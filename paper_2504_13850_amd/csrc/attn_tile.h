@@ -115,14 +115,15 @@ struct Tile<float, DP> {
     }
 };
 
-// 16 bytes of a row from column d on, zeros past D or where !ok.  vec: every row
-// starts 16-byte aligned and D is a whole number of chunks; else element by element.
-template <class T>
-__device__ __forceinline__ uint4 ld_chunk(const T* row, int d, int D, bool ok, bool vec) {
+// 16 bytes of a row from column d on, zeros past D or where !ok.  VEC: every row
+// starts 16-byte aligned, D is a whole number of chunks and a row stride is below
+// 2^24 bytes; else element by element.
+template <bool VEC, class T>
+__device__ __forceinline__ u32x4_t ld_chunk(const T* row, int d, int D, bool ok) {
     constexpr int N = 16 / sizeof(T);
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (vec) {
-        if (ok && d < D) u = *reinterpret_cast<const uint4*>(row + d);
+    u32x4_t u = {0u, 0u, 0u, 0u};
+    if (VEC) {
+        if (ok && d < D) u = *reinterpret_cast<const u32x4_t*>(row + d);
         return u;
     }
     T v[N];
@@ -131,12 +132,12 @@ __device__ __forceinline__ uint4 ld_chunk(const T* row, int d, int D, bool ok, b
     __builtin_memcpy(&u, v, 16);
     return u;
 }
-template <class T>
-__device__ __forceinline__ Frag<T> ld_frag(const T* row, int d, int D, bool ok, bool vec) {
+template <bool VEC, class T>
+__device__ __forceinline__ Frag<T> ld_frag(const T* row, int d, int D, bool ok) {
     Frag<T> f;
 #pragma unroll
     for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
-        const uint4 u = ld_chunk(row, d + c * (16 / (int)sizeof(T)), D, ok, vec);
+        const u32x4_t u = ld_chunk<VEC>(row, d + c * (16 / (int)sizeof(T)), D, ok);
         __builtin_memcpy((char*)&f.v + 16 * c, &u, 16);
     }
     return f;
@@ -144,25 +145,39 @@ __device__ __forceinline__ Frag<T> ld_frag(const T* row, int d, int D, bool ok, 
 
 // ROWS rows of a [rows][ld] operand through registers into an LDS tile: 256
 // threads, all loads of a tile issued together so that they fly while the
-// previous tile is in use.
-template <class T, int DP, int ROWS>
+// previous tile is in use.  Aligned rows (VEC) are read without a branch at 32-bit
+// offsets from a base that the scalar unit moves on; rows past the last one and
+// columns past D repeat the last row and chunk, which no result uses: their
+// probabilities are masked to zero, the other operand's columns are zero.
+template <class T, int DP, int ROWS, bool VEC>
 struct Stage {
     static constexpr int CPR = DP * (int)sizeof(T) / 16, N = ROWS * CPR / 256, EPC = 16 / (int)sizeof(T);
+    static constexpr int RS = 256 / CPR;  // rows between a thread's chunks
     static_assert(ROWS * CPR % 256 == 0, "whole chunks per thread");
-    uint4 u[N];
-    // Rows r0 .. of which those below n exist.
-    __device__ __forceinline__ void load(const T* base, int64_t ld, int r0, int n, int D, bool vec, int tid) {
+    u32x4_t u[N];
+    // Rows r0 .. of which those below n (more than r0) exist.
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int r0, int n, int D, int tid) {
+        if constexpr (VEC) {
+            const char* p = (const char*)(base + r0 * ld);
+            const uint32_t step = (uint32_t)(ld * sizeof(T)), last = (uint32_t)(n - 1 - r0);
+            const uint32_t col = 16 * min(tid % CPR, (D - 1) / EPC);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int x = tid + 256 * i, r = r0 + x / CPR;
-            u[i] = ld_chunk(base + (int64_t)r * ld, (x % CPR) * EPC, D, r < n, vec);
+            for (int i = 0; i < N; ++i)
+                u[i] = *reinterpret_cast<const u32x4_t*>(
+                    p + (__umul24(min((uint32_t)(tid / CPR + i * RS), last), step) + col));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = r0 + tid / CPR + i * RS;
+                u[i] = ld_chunk<false>(base + r * ld, (tid % CPR) * EPC, D, r < n);
+            }
         }
     }
     __device__ __forceinline__ void store(T* t, int tid) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int x = tid + 256 * i;
-            *reinterpret_cast<uint4*>(&t[Tile<T, DP>::idx(x / CPR, (x % CPR) * EPC)]) = u[i];
+            *reinterpret_cast<u32x4_t*>(&t[Tile<T, DP>::idx(x / CPR, (x % CPR) * EPC)]) = u[i];
         }
     }
 };
@@ -195,18 +210,24 @@ __device__ __forceinline__ void store_row(T* row, const f32x16* acc, float s, in
 // and s = scale S: tanh(x) = 1 - 2 / (e^2x + 1), whose absolute error of some 2^-23 is
 // far below a bf16 probability's rounding.  fp32 calls tanhf.
 struct ScoreK {
-    float mul;   // scale log2(e)
+    float mul;   // |scale| log2(e), not 0 so that it orders the scores and keeps -infinity
     float ck;    // 2 scale log2(e) / cap
     float cs;    // scale / cap
     float cl;    // cap log2(e)
 };
 __device__ __forceinline__ ScoreK score_k(const fo_attn& a) {
     ScoreK k;
-    k.mul = a.scale * kLog2e;
+    k.mul = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
     k.cs = a.cap > 0.f ? a.scale / a.cap : 0.f;
     k.ck = 2.f * kLog2e * k.cs;
     k.cl = a.cap * kLog2e;
     return k;
+}
+// Without a cap the sign of a negative scale goes into the row operand.
+template <class T>
+__device__ __forceinline__ void negate(Frag<T>& f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = -f.v[e];
 }
 // The capped score without its bias; slope = du / ds.
 template <class T>
@@ -233,9 +254,17 @@ __device__ __forceinline__ float bias_at(const fo_attn& a, int h, int n) {
 // radius before the whole tile lies beyond it, where its bias is one value.
 constexpr int kReach = 96;
 __host__ __device__ inline int lut_floats(const fo_attn& a) { return 2 * (a.radius + kReach) + 1; }
+// Calls f(n) for n = t, t + step, .. < count, in a loop that no lane leaves early:
+// one that lanes leave one by one had the compiler copy registers behind it
+// before it turned the lanes on again.
+template <class F>
+__device__ __forceinline__ void each(int t, int step, int count, F f) {
+    for (int n0 = 0; n0 < count; n0 += step)
+        if (n0 + t < count) f(n0 + t);
+}
 template <class T>
 __device__ __forceinline__ void fill_lut(float* lut, const fo_attn& a, int h, int tid) {
-    for (int x = tid; x < lut_floats(a); x += 256) lut[x] = bias_at<T>(a, h, x - a.radius - kReach);
+    each(tid, 256, lut_floats(a), [&](int x) { lut[x] = bias_at<T>(a, h, x - a.radius - kReach); });
 }
 
 // One past the last key that query i sees: a prefix of the keys for every mask.

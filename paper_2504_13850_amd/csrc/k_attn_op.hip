@@ -27,23 +27,23 @@ __global__ void __launch_bounds__(1024) bucket_sums(AttnArgs x, int parts) {
     const int h = blockIdx.x, W = 2 * a.radius + 1, tid = threadIdx.x, g4 = tid >> 8;
     const float* hist = x.hist + (int64_t)h * W;
     const int64_t step = (int64_t)a.heads * W;
-    for (int n = tid & 255; n < W; n += 256) {
+    each(tid & 255, 256, W, [&](int n) {
         float s = 0.f;
 #pragma unroll 8
         for (int p = g4; p < parts; p += 4) s += hist[p * step + n];
         sum[g4][n] = s;
         if (g4 == 0) of[n] = min(max(a.bucket[n], 0), a.n_buckets - 1);
-    }
+    });
     __syncthreads();
-    for (int n = tid; n < W; n += 1024) sum[0][n] = sum[0][n] + sum[1][n] + sum[2][n] + sum[3][n];
+    each(tid, 1024, W, [&](int n) { sum[0][n] = sum[0][n] + sum[1][n] + sum[2][n] + sum[3][n]; });
     __syncthreads();
-    for (int g = tid >> 5; g < a.n_buckets; g += 32) {
+    each(tid >> 5, 32, a.n_buckets, [&](int g) {
         float s = 0.f;
-        for (int n = tid & 31; n < W; n += 32) s += of[n] == g ? sum[0][n] : 0.f;
+        each(tid & 31, 32, W, [&](int n) { s += of[n] == g ? sum[0][n] : 0.f; });
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor(s, o);
         if ((tid & 31) == 0) ((T*)x.dtable)[(int64_t)g * a.heads + h] = from_f<T>(s);
-    }
+    });
 }
 
 // Joins the key slices of a row: one wave per row and head.
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(256) join_keys(AttnArgs x, BwdShape f) {
     const float* dv = dk + parts * step;
     T* outk = (T*)x.dk + (int64_t)(s.k0 + j) * a.k_ld + hk * a.k_hs;
     T* outv = (T*)x.dv + (int64_t)(s.k0 + j) * a.v_ld + hk * a.v_hs;
-    for (int c = lane; c < D; c += 64) {
+    each(lane, 64, D, [&](int c) {
         float sk = 0.f, sv = 0.f;
 #pragma unroll 4
         for (int p = 0; p < parts; ++p) {
@@ -105,12 +105,12 @@ __global__ void __launch_bounds__(256) join_keys(AttnArgs x, BwdShape f) {
         }
         outk[c] = from_f<T>(sk * a.scale);
         outv[c] = from_f<T>(sv * x.keep_scale);
-    }
+    });
 }
 
-// 16-byte aligned rows of a [rows][heads][dim] operand.
+// 16-byte aligned rows of a [rows][heads][dim] operand, their stride below 2^24 bytes.
 bool aligned_rows(const void* p, int64_t ld, int64_t hs, int64_t size) {
-    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && hs * size % 16 == 0;
+    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && hs * size % 16 == 0 && ld * size < (1 << 24);
 }
 bool vec_fwd(const AttnArgs& x) {
     const fo_attn& a = x.a;
