@@ -18,7 +18,7 @@ struct BwdShape {
     int wq, q_tiles;  // query kernel: waves side by side over rows, row tiles
     int wk, k_tiles;  // key kernel: the same over keys
     int h_parts, q_parts;  // and its cuts over a key head's heads and over the queries
-    bool vec;
+    bool vec, narrow;  // narrow: attn_narrow.h, tiles of 64
     float* part;  // partial dk, then dv, of the cuts: [h_parts q_parts][k_rows][kv_heads][D] each
 };
 

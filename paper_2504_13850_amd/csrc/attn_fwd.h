@@ -9,7 +9,7 @@ namespace fo {
 // of a workgroup are the heads of one key head's group, for one token.
 struct FwdShape {
     int wq, pack, row_tiles, splits;
-    bool vec;
+    bool vec, narrow;  // narrow: attn_narrow.h, row tiles of 64
     float *part, *ml;  // partial results of the key slices: [split][heads][q_rows][D], [..][2]
 };
 

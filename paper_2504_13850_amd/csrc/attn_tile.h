@@ -208,7 +208,8 @@ __device__ __forceinline__ void store_row(T* row, const f32x16* acc, float s, in
 // ------------------------------------------------------------------ scores, base 2
 // u log2(e) = S mul + add, or with a cap cl (1 - 2 w) + add, w = 1 / (e^(2 s / cap) + 1)
 // and s = scale S: tanh(x) = 1 - 2 / (e^2x + 1), whose absolute error of some 2^-23 is
-// far below a bf16 probability's rounding.  fp32 calls tanhf.
+// far below a bf16 probability's rounding.  fp32 takes the same form above 0.35 and
+// the series of tanh below, where the form would lose the leading digits.
 struct ScoreK {
     float mul;   // |scale| log2(e), not 0 so that it orders the scores and keeps -infinity
     float ck;    // 2 scale log2(e) / cap
@@ -237,7 +238,14 @@ __device__ __forceinline__ float capped(float S, const ScoreK& k, float* slope =
         if (slope) *slope = 4.f * fmaf(-w, w, w);
         return fmaf(w, -2.f * k.cl, k.cl);
     } else {
-        const float t = tanhf(S * k.cs);
+        const float y = S * k.cs, y2 = y * y, ay = fabsf(y);
+        float c = fmaf(y2, -1382.f / 155925.f, 62.f / 2835.f);
+        c = fmaf(y2, c, -17.f / 315.f);
+        c = fmaf(y2, c, 2.f / 15.f);
+        c = fmaf(y2, c, -1.f / 3.f);
+        const float low = fmaf(y * y2, c, y);
+        const float high = fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(ay * (2.f * kLog2e)) + 1.f), -2.f, 1.f);
+        const float t = ay < 0.35f ? low : __builtin_copysignf(high, y);
         if (slope) *slope = fmaf(-t, t, 1.f);
         return t * k.cl;
     }
@@ -263,8 +271,8 @@ __device__ __forceinline__ void each(int t, int step, int count, F f) {
         if (n0 + t < count) f(n0 + t);
 }
 template <class T>
-__device__ __forceinline__ void fill_lut(float* lut, const fo_attn& a, int h, int tid) {
-    each(tid, 256, lut_floats(a), [&](int x) { lut[x] = bias_at<T>(a, h, x - a.radius - kReach); });
+__device__ __forceinline__ void fill_lut(float* lut, const fo_attn& a, int h, int tid, int step = 256) {
+    each(tid, step, lut_floats(a), [&](int x) { lut[x] = bias_at<T>(a, h, x - a.radius - kReach); });
 }
 
 // One past the last key that query i sees: a prefix of the keys for every mask.

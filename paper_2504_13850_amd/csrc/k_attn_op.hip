@@ -3,8 +3,7 @@
 // gradient's sums.
 #include <algorithm>
 
-#include "attn_bwd.h"
-#include "attn_fwd.h"
+#include "attn_narrow.h"
 
 namespace fo {
 #define FO_EXTERN(T, D)                                                                              \
@@ -12,6 +11,12 @@ namespace fo {
     extern template fo_status attn_bwd_launch<T, D>(const AttnArgs&, const BwdShape&, hipStream_t)
 FO_EXTERN(bf16_t, 32); FO_EXTERN(bf16_t, 64); FO_EXTERN(bf16_t, 128);
 FO_EXTERN(float, 32); FO_EXTERN(float, 64); FO_EXTERN(float, 128);
+#undef FO_EXTERN
+#define FO_EXTERN(T, D)                                                                                \
+    extern template fo_status narrow_fwd_launch<T, D>(const AttnArgs&, const FwdShape&, hipStream_t);  \
+    extern template fo_status narrow_bwd_launch<T, D>(const AttnArgs&, const BwdShape&, hipStream_t)
+FO_EXTERN(bf16_t, 2); FO_EXTERN(bf16_t, 4); FO_EXTERN(bf16_t, 8);
+FO_EXTERN(float, 2); FO_EXTERN(float, 4); FO_EXTERN(float, 8);
 #undef FO_EXTERN
 
 namespace {
@@ -123,14 +128,17 @@ bool vec_fwd(const AttnArgs& x) {
 // a group as rows, so that a key head's cache is read once for all of them.
 // Where the row tiles do not fill the chip's 256 compute units twice, the keys
 // are cut into slices of at least 256 as well.
+constexpr int kNarrowDim = 8;  // the widest head of attn_narrow.h
+
 FwdShape fwd_shape(const fo_attn& a) {
     FwdShape f{};
     f.pack = a.max_q == 1;
+    f.narrow = a.head_dim <= kNarrowDim && a.max_q > 32;
     f.wq = f.pack || a.max_q <= 32 ? 1 : a.max_q <= 64 ? 2 : 4;
     const int64_t rows = f.pack ? a.heads / a.kv_heads : a.max_q;
-    f.row_tiles = (int)cdiv(rows, 32 * f.wq);
-    const int64_t wgs = (int64_t)f.row_tiles * (f.pack ? a.kv_heads : a.heads) * a.batch;
-    int64_t sp = cdiv(512, wgs);
+    f.row_tiles = (int)cdiv(rows, f.narrow ? kNarrowRows : 32 * f.wq);
+    const int64_t wgs = (int64_t)f.row_tiles * (f.pack ? a.kv_heads : a.heads) * a.batch / (f.narrow ? 4 : 1);
+    int64_t sp = cdiv(512, std::max<int64_t>(1, wgs));
     sp = std::min<int64_t>(sp, std::max<int64_t>(1, a.max_k / 256));
     f.splits = (int)std::min<int64_t>(sp, 64);
     return f;
@@ -138,13 +146,16 @@ FwdShape fwd_shape(const fo_attn& a) {
 
 BwdShape bwd_shape(const fo_attn& a) {
     BwdShape f{};
-    f.wq = a.max_q <= 32 ? 1 : a.max_q <= 64 ? 2 : 4;
+    f.narrow = a.head_dim <= kNarrowDim && a.max_q > 32 && a.max_k > 32;
+    if (f.narrow) f.wq = f.wk = kNarrowRows / 32;
+    else f.wq = a.max_q <= 32 ? 1 : a.max_q <= 64 ? 2 : 4;
     f.q_tiles = a.q_rows ? (int)cdiv(a.max_q, 32 * f.wq) : 0;
-    f.wk = a.max_k > 64 ? 4 : a.max_k > 32 || (a.dtype == FO_DT_F32 && a.head_dim > 64) ? 2 : 1;  // see min_wk
+    if (!f.narrow)
+        f.wk = a.max_k > 64 ? 4 : a.max_k > 32 || (a.dtype == FO_DT_F32 && a.head_dim > 64) ? 2 : 1;  // see min_wk
     f.k_tiles = a.k_rows ? (int)cdiv(a.max_k, 32 * f.wk) : 0;
     // The key kernel's work is cut until about 512 workgroups share it, each with
     // 512 query rows of one head or more, so that the cuts' sums stay a small part.
-    const int64_t wgs = std::max<int64_t>(1, (int64_t)f.k_tiles * a.kv_heads * a.batch), G = a.heads / a.kv_heads;
+    const int64_t wgs = std::max<int64_t>(1, (int64_t)f.k_tiles * a.kv_heads * a.batch / (f.narrow ? 4 : 1)), G = a.heads / a.kv_heads;
     const int64_t cuts = std::max<int64_t>(1, std::min<int64_t>({cdiv(512, wgs), G * a.max_q / 512, 64}));
     f.h_parts = (int)std::min(G, cuts);
     while (G % f.h_parts) --f.h_parts;
@@ -173,13 +184,27 @@ int64_t attn_workspace(const fo_attn& a, bool backward) {
 }
 
 template <class T>
+static fo_status fwd_narrow(const AttnArgs& x, const FwdShape& f, hipStream_t s) {
+    return x.a.head_dim <= 2   ? narrow_fwd_launch<T, 2>(x, f, s)
+           : x.a.head_dim <= 4 ? narrow_fwd_launch<T, 4>(x, f, s)
+                               : narrow_fwd_launch<T, 8>(x, f, s);
+}
+template <class T>
+static fo_status bwd_narrow(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
+    return x.a.head_dim <= 2   ? narrow_bwd_launch<T, 2>(x, f, s)
+           : x.a.head_dim <= 4 ? narrow_bwd_launch<T, 4>(x, f, s)
+                               : narrow_bwd_launch<T, 8>(x, f, s);
+}
+
+template <class T>
 static fo_status fwd(const AttnArgs& x, void* ws, hipStream_t s) {
     const fo_attn& a = x.a;
     FwdShape f = fwd_shape(a);
     f.vec = vec_fwd(x);
     f.part = (float*)ws;
     f.ml = f.part + (int64_t)f.splits * a.heads * a.q_rows * a.head_dim;
-    const fo_status st = a.head_dim <= 32   ? attn_fwd_launch<T, 32>(x, f, s)
+    const fo_status st = f.narrow           ? fwd_narrow<T>(x, f, s)
+                         : a.head_dim <= 32 ? attn_fwd_launch<T, 32>(x, f, s)
                          : a.head_dim <= 64 ? attn_fwd_launch<T, 64>(x, f, s)
                                             : attn_fwd_launch<T, 128>(x, f, s);
     if (st != FO_OK || f.splits == 1) return st;
@@ -202,7 +227,8 @@ static fo_status bwd(AttnArgs& x, float* ws, hipStream_t s) {
     x.hist = f.part + part_floats(a, f);
     f.vec = vec_fwd(x) && aligned_rows(x.dout, a.out_ld, a.out_hs, e) && aligned_rows(x.dq, a.q_ld, a.q_hs, e) &&
             aligned_rows(x.dk, a.k_ld, a.k_hs, e) && aligned_rows(x.dv, a.v_ld, a.v_hs, e);
-    const fo_status st = a.head_dim <= 32   ? attn_bwd_launch<T, 32>(x, f, s)
+    const fo_status st = f.narrow           ? bwd_narrow<T>(x, f, s)
+                         : a.head_dim <= 32 ? attn_bwd_launch<T, 32>(x, f, s)
                          : a.head_dim <= 64 ? attn_bwd_launch<T, 64>(x, f, s)
                                             : attn_bwd_launch<T, 128>(x, f, s);
     if (st != FO_OK) return st;

@@ -191,6 +191,37 @@ def test_lengths_and_empty_rows(dtype, mask, i):
           prefix=[(lk + 1) // 2 if b % 2 else 0 for b, (_, lk) in enumerate(lens)] if mask == 2 else None)
 
 
+# heads of a few columns: (dtype, lengths, heads, kv_heads, dim, mask, cap, radius, p, layout)
+NARROW = [
+    ("f32", (256, 16, 100, 65), 6, 6, 2, 1, 0.0, 1024, 0.1, "fused"), ("bf16", (200, 64), 4, 2, 8, 2, 3.0, 40, 0.2, "rows"),
+    ("f32", (300, 33), 4, 1, 5, 0, 2.0, 0, 0.0, "odd"), ("bf16", (129, 257), 3, 3, 3, 1, 0.0, None, 0.3, "heads"),
+    ("f32", (1100,), 2, 1, 1, 1, 0.0, 20, 0.0, "rows"), ("bf16", (64,), 12, 2, 2, 0, 0.0, 100, 0.0, "rows"),
+    ("f32", (700, 200), 8, 2, 8, 2, 0.0, 64, 0.1, "heads")]
+
+
+@pytest.mark.parametrize("i", range(len(NARROW)), ids=lambda i: "-".join(map(str, NARROW[i])).replace(" ", ""))
+def test_narrow_heads(i):
+    dtype, lens, heads, kv, dim, mask, cap, radius, p, layout = NARROW[i]
+    check(dtype=dtype, lens=tuple((n, n) for n in lens), heads=heads, kv_heads=kv, dim=dim, mask=mask, cap=cap,
+          radius=radius, p=p, layout=layout, prefix=[n // 3 for n in lens] if mask == 2 else None, gap=i % 3,
+          seed=300 + i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mask", [0, 1, 2])
+def test_narrow_lengths_and_empty_rows(dtype, mask):
+    lens = ((40, 5), (5, 70), (64, 1), (1, 1), (33, 0), (0, 9), (130, 64), (60, 2000))
+    check(dtype=dtype, lens=lens, heads=4, kv_heads=2, dim=4, mask=mask, cap=3.0, radius=9, p=0.3, gap=1, seed=320,
+          prefix=[(lk + 1) // 2 if b % 2 else 0 for b, (_, lk) in enumerate(lens)] if mask == 2 else None)
+
+
+def test_negative_and_zero_scale():
+    for k, scale in enumerate((-0.3, 0.0)):
+        for cap in (0.0, 2.0):
+            check(dtype="bf16", lens=((70, 70),), heads=2, dim=64, mask=1, cap=cap, scale=scale, radius=8, seed=330 + k)
+            check(dtype="f32", lens=((70, 70),), heads=2, dim=6, mask=1, cap=cap, scale=scale, seed=340 + k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hide", ["inf", "lowest"])
 def test_hidden_distances(dtype, hide):
