@@ -36,8 +36,10 @@ constexpr int bwd_kb(int wn) { return wn == 4 ? 64 : 32 * (4 / wn); }
 // Scores S -> u log2(e) + add, and du/ds.
 template <class T, bool CAP>
 __device__ __forceinline__ void to_exponent(f32x16& S, float* slope, const ScoreK& k, float add) {
+    if (CAP) cap_scores<T, 16>(S, k, slope);
+    const float mul = CAP ? 1.f : k.mul;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) S[r] = CAP ? capped<T>(S[r], k, &slope[r]) + add : fmaf(S[r], k.mul, add);
+    for (int r = 0; r < 16; ++r) S[r] = fmaf(S[r], mul, add);
 }
 template <class F>
 __device__ __forceinline__ void near_bias(f32x16& S, F f) {

@@ -117,24 +117,24 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
         // distances of the wave's rows to this tile: [n_lo, n_hi]
         const int n_lo = j0 - (f.pack ? 0 : iw + 31) - off, n_hi = j0 + 32 * KT - 1 - (f.pack ? 0 : iw) - off;
         const bool near = EXTRA && bias && n_lo < a.radius && n_hi > -a.radius;
-        const float add0 = !EXTRA || !bias ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
+        const float add0 = !EXTRA || !bias || near ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
         float mul = sc.mul, add = add0;
-        if (CAP || near) {  // x itself takes S's place
+        if (CAP) {
+#pragma unroll
+            for (int c = 0; c < KT; ++c) cap_scores<T, 16>(S[c], sc, nullptr);
+            mul = 1.f;
+        }
+        if (near) {  // x itself takes S's place
             const int base = j0 + 4 * lh - qi - off;
 #pragma unroll
             for (int c = 0; c < KT; ++c)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int j = 32 * c + 8 * (r >> 2) + (r & 3);
-                    float v = CAP ? capped<T>(S[c][r], sc) : S[c][r] * sc.mul;
-                    if (near)
-                        v += f.pack ? bias_at<T>(a, ok ? head : h0, base + j) : lut[base + j + a.radius + kReach];
-                    else
-                        v += add0;
-                    S[c][r] = v;
+                    const float v = f.pack ? bias_at<T>(a, ok ? head : h0, base + j) : lut[base + j + a.radius + kReach];
+                    S[c][r] = fmaf(S[c][r], mul, v);
                 }
             mul = 1.f;
-            add = 0.f;
         }
         if (j0 + 32 * KT > wave_all) {  // some row does not see the whole tile
             const int left = lim - j0 - 4 * lh;

@@ -31,10 +31,12 @@ __device__ __forceinline__ float dot_narrow(const float* x, const float* y) {
     for (int d = 1; d < DN; ++d) s = fmaf(x[d], y[d], s);
     return s;
 }
-// u log2(e) without its bias, and du/ds
-template <class T, bool CAP>
-__device__ __forceinline__ float narrow_score(float s, const ScoreK& k, float mul, float* slope) {
-    return CAP ? capped<T>(s, k, slope) : s * mul;
+// Scores -> u log2(e) + add, and du/ds.
+template <class T, bool CAP, int N>
+__device__ __forceinline__ void narrow_exponent(float (&S)[N], float* slope, const ScoreK& k, float mul, float add) {
+    if (CAP) cap_scores<T, N>(S, k, slope);
+#pragma unroll
+    for (int r = 0; r < N; ++r) S[r] = fmaf(S[r], CAP ? 1.f : mul, add);
 }
 
 // Rows of one wave: 64 queries of head h (fwd, dq) or 64 keys of head hk.
@@ -97,10 +99,10 @@ __global__ void __launch_bounds__(256) narrow_fwd(AttnArgs x, FwdShape f) {
             const int n_lo = j0 - (i0 + 63) - off, n_hi = j0 + 15 - i0 - off;
             const bool near = EXTRA && bias && n_lo < a.radius && n_hi > -a.radius;
             const float add0 = !EXTRA || !bias || near ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
-            float S[16], slope;
+            float S[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                S[r] = narrow_score<T, CAP>(dot_narrow<DN>(q, &kv[(16 * g + r) * 2 * DN]), sc, mul, &slope) + add0;
+            for (int r = 0; r < 16; ++r) S[r] = dot_narrow<DN>(q, &kv[(16 * g + r) * 2 * DN]);
+            narrow_exponent<T, CAP, 16>(S, nullptr, sc, mul, add0);
             if (near) {
                 const float* at = &lut[j0 - qi - off + a.radius + kReach];
 #pragma unroll
@@ -238,19 +240,24 @@ __global__ void __launch_bounds__(256) narrow_dq(AttnArgs x, BwdShape f) {
                     for (int e = 0; e < 8; ++e) bits[hh] |= (half_of(c, e) >= x.thr ? 1u : 0u) << e;
                 }
             }
+            float S[16], slope[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) S[r] = dot_narrow<DN>(q, &kv[(16 * gr + r) * 2 * DN]);
+            narrow_exponent<T, CAP, 16>(S, slope, sc, mul, add0 - lse);
+            if (near) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) S[r] += at[r];
+            }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float* kr = &kv[(16 * gr + r) * 2 * DN];
-                float slope = 1.f;
-                float u = narrow_score<T, CAP>(dot_narrow<DN>(q, kr), sc, mul, &slope) + add0;
-                if (near) u += at[r];
-                float p = __builtin_amdgcn_exp2f(u - lse);
+                float p = __builtin_amdgcn_exp2f(S[r]);
                 if (masked) p = j0 + r < lim ? p : 0.f;
                 float dp = dot_narrow<DN>(g, kr + DN);
                 if (EXTRA && x.thr) dp = (bits[(r >> 2) & 1] >> ((r & 3) | ((r >> 1) & 4))) & 1 ? dp * x.keep_scale : 0.f;
                 const float du = p * (dp - dl);
                 err += du;
-                const float ds = CAP ? du * slope : du, ps = CAP ? p * slope : p;
+                const float ds = CAP ? du * slope[r] : du, ps = CAP ? p * slope[r] : p;
 #pragma unroll
                 for (int d = 0; d < DN; ++d) {
                     dQ[d] = fmaf(ds, kr[d], dQ[d]);
@@ -366,16 +373,19 @@ __global__ void __launch_bounds__(256) narrow_dkv(AttnArgs x, BwdShape f) {
             const bool far = !EXTRA || !bias || n_lo >= R || n_hi <= -R, high = n_lo >= R;
             const float add0 = !EXTRA || !bias ? 0.f : high ? far_hi : far_lo;
             const bool masked = it < all;
-            // four rows at a time; rows past the last have P = 0
-            for (int r4 = 0; r4 < 64 && it + r4 < s.nq; r4 += 4)
+            // eight rows at a time; rows past the last have P = 0
+            for (int r8 = 0; r8 < 64 && it + r8 < s.nq; r8 += 8) {
+              float S[8], slope[8];
 #pragma unroll
-            for (int r = r4; r < r4 + 4; ++r) {
+              for (int r = 0; r < 8; ++r) S[r] = dot_narrow<DN>(k, &qg[(r8 + r) * QW]);
+              narrow_exponent<T, CAP, 8>(S, slope, sc, mul, far ? add0 : 0.f);
+#pragma unroll
+              for (int r0 = 0; r0 < 8; ++r0) {
+                const int r = r8 + r0;
                 const float* qr = &qg[r * QW];
-                float slope = 1.f;
-                float u = narrow_score<T, CAP>(dot_narrow<DN>(k, qr), sc, mul, &slope);
                 const int at = min(max(j - it - r - off, -R), R) + R + kReach;
-                if (EXTRA && bias) u += far ? add0 : lut[at];
-                float p = __builtin_amdgcn_exp2f(u - qr[2 * DN]);
+                if (EXTRA && bias && !far) S[r0] += lut[at];
+                float p = __builtin_amdgcn_exp2f(S[r0] - qr[2 * DN]);
                 if (masked) p = it + r >= first ? p : 0.f;
                 float dp = dot_narrow<DN>(v, qr + DN), pd = p;
                 if (EXTRA && x.thr) {
@@ -397,12 +407,13 @@ __global__ void __launch_bounds__(256) narrow_dkv(AttnArgs x, BwdShape f) {
                     }
                     wave_sync();
                 }
-                const float ds = CAP ? du * slope : du;
+                const float ds = CAP ? du * slope[r0] : du;
 #pragma unroll
                 for (int d = 0; d < DN; ++d) {
                     dK[d] = fmaf(ds, qr[d], dK[d]);
                     dV[d] = fmaf(pd, qr[DN + d], dV[d]);
                 }
+              }
             }
         }
         if (bias) {
