@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -539,34 +540,41 @@ def _same(what, ref, *tensors):
             raise FoError(FO_EINVAL, f"{what}: operands of one type with a contiguous last dimension")
 
 
+# fo_attn as one packed record: building it field by field takes several times as long
+_ATTN = struct.Struct("@7i2q4P8q2fi3P2ifQI0q")
+assert _ATTN.size == C.sizeof(fo_attn)
+
+
 def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: int, scale=None, cap: float = 0.0,
               mask: int = FO_ATTN_FULL, prefix=None, table=None, bucket=None, p: float = 0.0, seed: int = 0,
               offset: int = 0) -> fo_attn:
     """The record of an attention over q [rows, heads, dim], k and v [rows, kv_heads, dim] and out like q, whose
     rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  The record holds addresses: the bounds,
     prefix, table and bucket tensors have to live until the calls that use it have run."""
-    dt, batch = _dtype(q), q_begin.numel()
+    dt, ty, batch, i32 = _dtype(q), q.dtype, q_begin.numel(), _INT32[0]
     rows, heads, dim = shape = q.shape
     k_rows, kv_heads, k_dim = k_shape = k.shape
     if k_dim != dim or v.shape != k_shape or out.shape != shape:
         raise FoError(FO_EINVAL, f"fo_attn: q {tuple(shape)}, k {tuple(k_shape)}, v {tuple(v.shape)}, "
                                  f"out {tuple(out.shape)}")
-    _same("fo_attn", q, q, k, v, out, table)
-    for t in (q_begin, q_end, k_begin, k_end, prefix):
-        if t is not None and (t.dtype != _INT32[0] or t.numel() != batch or (batch > 1 and t.stride() != (1,))):
+    (ql, qh, q1), (kl, kh, k1), (vl, vh, v1), (ol, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    if k.dtype != ty or v.dtype != ty or out.dtype != ty or (dim > 1 and (q1 != 1 or k1 != 1 or v1 != 1 or o1 != 1)):
+        raise FoError(FO_EINVAL, "fo_attn: operands of one type with a contiguous last dimension")
+    for t in (q_begin, q_end, k_begin, k_end) if prefix is None else (q_begin, q_end, k_begin, k_end, prefix):
+        if t.dtype != i32 or t.numel() != batch or not t.is_contiguous():
             raise FoError(FO_EINVAL, "fo_attn: sequence bounds and prefix are int32, one for each sequence")
-    n_buckets = radius = 0
-    if table is not None:
-        n_buckets, radius = table.shape[0], 0 if bucket is None else bucket.numel() // 2
-        if (table.shape[1:] != (heads,) or not table.is_contiguous() or bucket is None or bucket.numel() % 2 == 0
-                or bucket.dtype != _INT32[0] or not bucket.is_contiguous()):
+    n_buckets = radius = table_at = bucket_at = 0
+    if table is not None or bucket is not None:
+        if (table is None or bucket is None or table.dtype != ty or table.dim() != 2 or table.shape[1] != heads
+                or not table.is_contiguous() or bucket.numel() % 2 == 0 or bucket.dtype != i32
+                or not bucket.is_contiguous()):
             raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the int32 buckets of 2 radius + 1 "
                                      "distances")
-    (ql, qh, _), (kl, kh, _), (vl, vh, _), (ol, oh, _) = q.stride(), k.stride(), v.stride(), out.stride()
-    return fo_attn(dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(),
-                   q_end.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh,
-                   dim ** -0.5 if scale is None else scale, cap, mask, _dptr(prefix), _dptr(table), _dptr(bucket),
-                   n_buckets, radius, p, seed, offset)
+        n_buckets, radius, table_at, bucket_at = table.shape[0], bucket.numel() // 2, table.data_ptr(), bucket.data_ptr()
+    return fo_attn.from_buffer_copy(_ATTN.pack(
+        dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(), q_end.data_ptr(),
+        k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh, dim ** -0.5 if scale is None else scale,
+        cap, mask, 0 if prefix is None else prefix.data_ptr(), table_at, bucket_at, n_buckets, radius, p, seed, offset))
 
 
 def _bytes(ws) -> int:
@@ -588,11 +596,12 @@ def fo_attn_fwd(attn: fo_attn, q, k, v, out, lse=None, workspace=None, stream=No
 
 def fo_attn_bwd(attn: fo_attn, q, k, v, out, lse, dout, dq, dk, dv, dtable=None, workspace=None, stream=None):
     """dout has out's strides; dq, dk and dv have those of q, k and v."""
-    _same("fo_attn_bwd", q, dout, dq, dk, dv, dtable)
+    ty = q.dtype
     for a, b in ((out, dout), (q, dq), (k, dk), (v, dv)):
-        if a.shape != b.shape or any(n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride())):
-            raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the shapes and strides of what they belong to")
-    if dtable is not None and (not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
+        if b.dtype != ty or a.shape != b.shape or (a.stride() != b.stride() and any(
+                n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride()))):
+            raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes and strides of what they belong to")
+    if dtable is not None and (dtable.dtype != ty or not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
         raise FoError(FO_EINVAL, "fo_attn_bwd: dtable has the table's shape")
     _check(lib().fo_attn_bwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
                              dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _dptr(dtable),

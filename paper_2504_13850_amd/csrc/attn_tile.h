@@ -82,17 +82,18 @@ struct Tile<bf16_t, DP> {
     static __device__ __forceinline__ Frag<bf16_t> frag_row(const bf16_t* t, int row0, int col0, int lane) {
         return {*reinterpret_cast<const bf16x8_t*>(&t[idx(row0 + (lane & 31), col0 + 8 * (lane >> 5))])};
     }
-    // Lane rows are tile columns col0 + l % 32, k are 16 tile rows from row0 in the
-    // accumulators' order: two transpose reads (ds_read_b64_tr_b16: within each group
+    // Lane rows are tile columns col0 + l % 32, k are 16 tile rows from row0, in the
+    // accumulators' order or in their own (PLAIN): two transpose reads (ds_read_b64_tr_b16: within each group
     // of 16 lanes, lane i receives element i mod 4 of the 8 bytes addressed by lane
     // 4 j + i / 4, j = 0..3).
+    template <bool PLAIN = false>
     static __device__ __forceinline__ Frag<bf16_t> frag_col(const bf16_t* t, int row0, int col0, int lane) {
         const int g = lane >> 4, s = lane & 15, col = col0 + 16 * (g & 1) + 4 * (s & 3);
         s16x4_t v[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
             v[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4_t*)(t + idx(row0 + 4 * (lane >> 5) + 8 * r + (s >> 2), col)));
+                (lds_s16x4_t*)(t + idx(row0 + (PLAIN ? 8 : 4) * (lane >> 5) + (PLAIN ? 4 : 8) * r + (s >> 2), col)));
         const s16x8_t o = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
         return {__builtin_bit_cast(bf16x8_t, o)};
     }
@@ -106,11 +107,13 @@ struct Tile<float, DP> {
         const f32x4 a = p[0], b = p[1];
         return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
     }
+    template <bool PLAIN = false>
     static __device__ __forceinline__ Frag<float> frag_col(const float* t, int row0, int col0, int lane) {
         Frag<float> f;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            f.v[e] = t[idx(row0 + 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2), col0 + (lane & 31))];
+            f.v[e] = t[idx(row0 + (PLAIN ? 8 * (lane >> 5) + e : 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2)),
+                           col0 + (lane & 31))];
         return f;
     }
 };
@@ -143,17 +146,17 @@ __device__ __forceinline__ Frag<T> ld_frag(const T* row, int d, int D, bool ok) 
     return f;
 }
 
-// ROWS rows of a [rows][ld] operand through registers into an LDS tile: 256
-// threads, all loads of a tile issued together so that they fly while the
+// ROWS rows of a [rows][ld] operand through registers into an LDS tile, all
+// loads of a tile issued together so that they fly while the
 // previous tile is in use.  Aligned rows (VEC) are read without a branch at 32-bit
 // offsets from a base that the scalar unit moves on; rows past the last one and
 // columns past D repeat the last row and chunk, which no result uses: their
 // probabilities are masked to zero, the other operand's columns are zero.
-template <class T, int DP, int ROWS, bool VEC>
+template <class T, int DP, int ROWS, bool VEC, int THREADS = 256>
 struct Stage {
-    static constexpr int CPR = DP * (int)sizeof(T) / 16, N = ROWS * CPR / 256, EPC = 16 / (int)sizeof(T);
-    static constexpr int RS = 256 / CPR;  // rows between a thread's chunks
-    static_assert(ROWS * CPR % 256 == 0, "whole chunks per thread");
+    static constexpr int CPR = DP * (int)sizeof(T) / 16, N = ROWS * CPR / THREADS, EPC = 16 / (int)sizeof(T);
+    static constexpr int RS = THREADS / CPR;  // rows between a thread's chunks
+    static_assert(ROWS * CPR % THREADS == 0, "whole chunks per thread");
     u32x4_t u[N];
     // Rows r0 .. of which those below n (more than r0) exist.
     __device__ __forceinline__ void load(const T* base, int64_t ld, int r0, int n, int D, int tid) {
@@ -173,10 +176,16 @@ struct Stage {
             }
         }
     }
+    // Zeros in the columns past D, for tiles that meet another tile's there.
+    __device__ __forceinline__ void clear_past(int D, int tid) {
+        const bool out = (tid % CPR) * EPC >= D;
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = out ? u32x4_t{0u, 0u, 0u, 0u} : u[i];
+    }
     __device__ __forceinline__ void store(T* t, int tid) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int x = tid + 256 * i;
+            const int x = tid + THREADS * i;
             *reinterpret_cast<u32x4_t*>(&t[Tile<T, DP>::idx(x / CPR, (x % CPR) * EPC)]) = u[i];
         }
     }

@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "attn_narrow.h"
+#include "attn_small.h"
 
 namespace fo {
 #define FO_EXTERN(T, D)                                                                              \
@@ -17,6 +18,9 @@ FO_EXTERN(float, 32); FO_EXTERN(float, 64); FO_EXTERN(float, 128);
     extern template fo_status narrow_bwd_launch<T, D>(const AttnArgs&, const BwdShape&, hipStream_t)
 FO_EXTERN(bf16_t, 2); FO_EXTERN(bf16_t, 4); FO_EXTERN(bf16_t, 8);
 FO_EXTERN(float, 2); FO_EXTERN(float, 4); FO_EXTERN(float, 8);
+#undef FO_EXTERN
+#define FO_EXTERN(T, D) extern template fo_status small_bwd_launch<T, D>(const AttnArgs&, hipStream_t)
+FO_EXTERN(bf16_t, 32); FO_EXTERN(bf16_t, 64); FO_EXTERN(bf16_t, 128); FO_EXTERN(float, 32); FO_EXTERN(float, 64);
 #undef FO_EXTERN
 
 namespace {
@@ -218,6 +222,33 @@ fo_status launch_attn_op_fwd(const AttnArgs& x, void* ws, hipStream_t s) {
 }
 
 template <class T>
+static fo_status bias_gradient(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
+    if (!x.a.table) return FO_OK;
+    bucket_sums<T><<<(unsigned)x.a.heads, 1024, 0, s>>>(x, f.q_parts * f.k_tiles * x.a.batch);
+    FO_LAUNCHED();
+    return FO_OK;
+}
+
+// One launch for sequences that a workgroup holds whole (attn_small.h).
+static bool short_sequences(const fo_attn& a) {
+    return a.max_q >= 1 && a.max_q <= 128 && a.max_k >= 1 && a.max_k <= 128 && a.heads == a.kv_heads;
+}
+template <class T>
+static bool small_holds(const fo_attn& a) {
+    if (a.head_dim <= 32) return small_fits<T, 32>(a);
+    if (a.head_dim <= 64) return small_fits<T, 64>(a);
+    if constexpr (sizeof(T) == 2) return small_fits<T, 128>(a);
+    return false;  // fp32 rows of 128 do not fit
+}
+template <class T>
+static fo_status run_small(const AttnArgs& x, hipStream_t s) {
+    if (x.a.head_dim <= 32) return small_bwd_launch<T, 32>(x, s);
+    if constexpr (sizeof(T) == 2)
+        if (x.a.head_dim > 64) return small_bwd_launch<T, 128>(x, s);
+    return small_bwd_launch<T, 64>(x, s);
+}
+
+template <class T>
 static fo_status bwd(AttnArgs& x, float* ws, hipStream_t s) {
     const fo_attn& a = x.a;
     const int64_t e = sizeof(T);
@@ -227,6 +258,12 @@ static fo_status bwd(AttnArgs& x, float* ws, hipStream_t s) {
     x.hist = f.part + part_floats(a, f);
     f.vec = vec_fwd(x) && aligned_rows(x.dout, a.out_ld, a.out_hs, e) && aligned_rows(x.dq, a.q_ld, a.q_hs, e) &&
             aligned_rows(x.dk, a.k_ld, a.k_hs, e) && aligned_rows(x.dv, a.v_ld, a.v_hs, e);
+    if (f.vec && a.q_rows && a.k_rows && short_sequences(a) && small_holds<T>(a)) {
+        f.k_tiles = f.h_parts = f.q_parts = 1;
+        const fo_status st = run_small<T>(x, s);
+        if (st != FO_OK) return st;
+        return bias_gradient<T>(x, f, s);
+    }
     const fo_status st = f.narrow           ? bwd_narrow<T>(x, f, s)
                          : a.head_dim <= 32 ? attn_bwd_launch<T, 32>(x, f, s)
                          : a.head_dim <= 64 ? attn_bwd_launch<T, 64>(x, f, s)
@@ -236,11 +273,7 @@ static fo_status bwd(AttnArgs& x, float* ws, hipStream_t s) {
         join_keys<T><<<(unsigned)cdiv((int64_t)a.batch * a.max_k * a.kv_heads, 4), 256, 0, s>>>(x, f);
         FO_LAUNCHED();
     }
-    if (a.table) {
-        bucket_sums<T><<<(unsigned)a.heads, 1024, 0, s>>>(x, f.q_parts * f.k_tiles * a.batch);
-        FO_LAUNCHED();
-    }
-    return FO_OK;
+    return bias_gradient<T>(x, f, s);
 }
 
 fo_status launch_attn_op_bwd(AttnArgs& x, void* ws, hipStream_t s) {

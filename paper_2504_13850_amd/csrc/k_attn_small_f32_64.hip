@@ -1,0 +1,6 @@
+// Attention backward for short sequences, f32, head widths up to 64.
+#include "attn_small.h"
+
+namespace fo {
+template fo_status small_bwd_launch<float, 64>(const AttnArgs&, hipStream_t);
+}  // namespace fo

@@ -215,6 +215,23 @@ def test_narrow_lengths_and_empty_rows(dtype, mask):
           prefix=[(lk + 1) // 2 if b % 2 else 0 for b, (_, lk) in enumerate(lens)] if mask == 2 else None)
 
 
+# sequences that one workgroup holds: (dtype, lengths, heads, dim, mask, cap, radius, p)
+SHORT = [("bf16", ((128, 128), (1, 128), (128, 1), (33, 97)), 3, 64, 0, 0.0, 50, 0.2),
+         ("bf16", ((64, 64), (17, 3), (0, 40), (50, 0), (31, 33)), 4, 128, 1, 3.0, 64, 0.1),
+         ("f32", ((128, 100), (65, 64), (10, 128)), 2, 64, 2, 2.0, 1024, 0.3),
+         ("f32", ((64, 64), (1, 1), (40, 20), (2, 64)), 5, 20, 1, 0.0, 0, 0.0),
+         ("bf16", ((127, 65), (96, 128)), 2, 48, 2, 0.0, None, 0.0), ("f32", ((90, 90),), 2, 100, 0, 0.0, 20, 0.1),
+         ("bf16", ((100, 128), (128, 90)), 2, 80, 1, 50.0, 1024, 0.0)]
+
+
+@pytest.mark.parametrize("i", range(len(SHORT)), ids=lambda i: "-".join(map(str, SHORT[i])).replace(" ", ""))
+def test_short_sequences(i):
+    dtype, lens, heads, dim, mask, cap, radius, p = SHORT[i]
+    check(dtype=dtype, lens=lens, heads=heads, dim=dim, mask=mask, cap=cap, radius=radius, p=p, layout=("rows", "heads")[i % 2],
+          gap=1 + i % 2, seed=400 + i,
+          prefix=[(lk + 1) // 2 if b % 2 else 0 for b, (_, lk) in enumerate(lens)] if mask == 2 else None)
+
+
 def test_negative_and_zero_scale():
     for k, scale in enumerate((-0.3, 0.0)):
         for cap in (0.0, 2.0):
