@@ -56,7 +56,8 @@ typedef struct {
     int32_t dtype;                       /* FO_DT_*                                            */
     int32_t batch, heads, kv_heads;      /* kv_heads divides heads                             */
     int32_t head_dim;                    /* 1..128                                             */
-    int32_t max_q, max_k;                /* upper bounds of the sequences' lengths             */
+    int32_t max_q, max_k;                /* upper bounds of the sequences' lengths: queries,
+                                          * and keys of a backward pass, up to 2^20; keys 2^30 */
     int64_t q_rows, k_rows;              /* rows of q and out, of k and v                      */
     /* Sequence b: query rows [q_begin[b], q_end[b]), key rows [k_begin[b],
      * k_end[b]), device int32[batch] each.  Rows packed by offsets cu[batch + 1]:

@@ -31,8 +31,8 @@ fo_status check_attn(const fo_attn* a) {
              "fo_attn: batch=%d heads=%d kv_heads=%d", a->batch, a->heads, a->kv_heads);
     FO_CHECK(a->batch <= 65535 && a->heads <= 65535, "fo_attn: batch=%d heads=%d beyond 65535", a->batch, a->heads);
     FO_CHECK(a->head_dim >= 1 && a->head_dim <= 128, "fo_attn: head_dim=%d outside [1, 128]", a->head_dim);
-    constexpr int32_t kMaxLen = 1 << 30;
-    FO_CHECK(a->max_q >= 0 && a->max_k >= 0 && a->max_q <= kMaxLen && a->max_k <= kMaxLen,
+    constexpr int32_t kMaxQ = 1 << 20, kMaxK = 1 << 30;  // 32-row tiles in a launch's third dimension
+    FO_CHECK(a->max_q >= 0 && a->max_k >= 0 && a->max_q <= kMaxQ && a->max_k <= kMaxK,
              "fo_attn: max_q=%d max_k=%d", a->max_q, a->max_k);
     FO_CHECK(a->q_rows >= 0 && a->k_rows >= 0 && a->q_rows <= INT32_MAX && a->k_rows <= INT32_MAX,
              "fo_attn: q_rows=%lld k_rows=%lld", (long long)a->q_rows, (long long)a->k_rows);
@@ -110,6 +110,7 @@ extern "C" fo_status fo_attn_bwd(const fo_attn* a, const void* q, const void* k,
     if ((st = check_operands(a, q, k, v, out, workspace, workspace_bytes, true)) != FO_OK) return st;
     const int64_t e = elem_size(a->dtype);
     FO_CHECK((a->q_rows == 0 || (lse && dout && dq)) && (a->k_rows == 0 || (dk && dv)), "fo_attn_bwd: NULL operand");
+    FO_CHECK(a->max_k <= 1 << 20, "fo_attn_bwd: max_k=%d", a->max_k);
     FO_CHECK(!a->table == !dtable, "fo_attn_bwd: dtable goes with the table");
     FO_CHECK(aligned(lse, 4) && aligned(dout, e) && aligned(dq, e) && aligned(dk, e) && aligned(dv, e) &&
              aligned(dtable, e), "fo_attn_bwd: unaligned operand");

@@ -15,6 +15,7 @@
 namespace fo {
 
 struct BwdShape {
+    int group;        // heads per key head
     int wq, q_tiles;  // query kernel: waves side by side over rows, row tiles
     int wk, k_tiles;  // key kernel: the same over keys
     int h_parts, q_parts;  // and its cuts over a key head's heads and over the queries
@@ -68,10 +69,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 31, lh = lane >> 5;
     const int wq = w % WQ, wk = w / WQ;
     const int D = a.head_dim;
-    int id = blockIdx.x;
-    const int h = id % a.heads, hk = h / (a.heads / a.kv_heads);
-    id /= a.heads;
-    const int b = id % a.batch, i0 = (f.q_tiles - 1 - id / a.batch) * 32 * WQ;
+    const int h = blockIdx.x, hk = f.group > 1 ? h / f.group : h, b = blockIdx.y;
+    const int i0 = (f.q_tiles - 1 - blockIdx.z) * 32 * WQ;  // longest first
     const Span s = span_of(a, b);
     if (i0 >= s.nq) return;
     const int pre = a.mask == FO_ATTN_PREFIX ? a.prefix[b] : 0, off = s.nk - s.nq;
@@ -268,15 +267,18 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
     const fo_attn& a = x.a;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 31, lh = lane >> 5;
     const int wn = w % WN, wk = w / WN;
-    const int D = a.head_dim, G = a.heads / a.kv_heads, R = a.radius;
-    int id = blockIdx.x;
-    const int hk = id % a.kv_heads;
-    id /= a.kv_heads;
-    const int b = id % a.batch;
-    id /= a.batch;
-    const int parts = f.h_parts * f.q_parts, part = id % parts, qp = part / f.h_parts, kt = id / parts;
-    const int j0 = kt * 32 * WN, hb = (G + f.h_parts - 1) / f.h_parts;
-    const int h0 = min(part % f.h_parts * hb, G), h1 = min(h0 + hb, G);  // the workgroup's heads of the group
+    const int D = a.head_dim, G = f.group, R = a.radius;
+    const int hk = blockIdx.x, b = blockIdx.y, parts = f.h_parts * f.q_parts;
+    int kt = blockIdx.z, part = 0, qp = 0, h0 = 0, h1 = G;  // h0, h1: the workgroup's heads of the group
+    if (parts > 1) {
+        part = kt % parts;
+        kt /= parts;
+        qp = part / f.h_parts;
+        const int hb = (G + f.h_parts - 1) / f.h_parts;
+        h0 = min(part % f.h_parts * hb, G);
+        h1 = min(h0 + hb, G);
+    }
+    const int j0 = kt * 32 * WN;
     float* hist = EXTRA && a.table
                       ? x.hist + ((((int64_t)qp * f.k_tiles + kt) * a.batch + b) * a.heads + hk * G) * (2 * R + 1)
                       : nullptr;
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
     const int wave_from = jw < s.nk ? first_of(jw) : 0x7fffffff;
     const int wave_all = jw + 32 <= s.nk ? first_of(jw + 31) : 0x7fffffff;  // all 32 keys are seen from here on
     int t0 = min(first_of(j0), s.nq) / QB, t1 = (s.nq + QB - 1) / QB;
-    {
+    if (f.q_parts > 1) {
         const int per = (t1 - t0 + f.q_parts - 1) / f.q_parts;
         t0 = min(t0 + qp * per, t1);
         t1 = min(t0 + per, t1);
@@ -513,7 +515,7 @@ fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
     const bool cap = a.cap > 0.f, extra = a.table || x.thr;  // EXTRA: a bias or dropout
     const unsigned lds = a.table ? 4 * lut_floats(a) : 0;
     if (f.q_tiles) {
-        const unsigned n = (unsigned)((int64_t)f.q_tiles * a.heads * a.batch);
+        const dim3 n(a.heads, a.batch, f.q_tiles);
 #define FO_DQ(W, CAP, EXTRA, VEC) attn_dq_kernel<T, DP, W, CAP, EXTRA, VEC><<<n, 256, lds, s>>>(x, f)
 #define FO_DQ_W(CAP, EXTRA)                                    \
     {                                                          \
@@ -532,7 +534,7 @@ fo_status attn_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s) {
         FO_LAUNCHED();
     }
     if (f.k_tiles) {
-        const unsigned n = (unsigned)((int64_t)f.k_tiles * f.h_parts * f.q_parts * a.kv_heads * a.batch);
+        const dim3 n(a.kv_heads, a.batch, f.k_tiles * f.h_parts * f.q_parts);
 #define FO_DKV(W, CAP, EXTRA, VEC) attn_dkv_kernel<T, DP, W, CAP, EXTRA, VEC><<<n, 256, 5 * lds, s>>>(x, f)
 #define FO_DKV_W(CAP, EXTRA)                                                  \
     {                                                                         \

@@ -8,7 +8,7 @@ namespace fo {
 // A launch's shape.  rows: query rows of one workgroup (32 WQ); pack: the rows
 // of a workgroup are the heads of one key head's group, for one token.
 struct FwdShape {
-    int wq, pack, row_tiles, splits;
+    int wq, pack, row_tiles, splits, group;  // group: heads per key head
     bool vec, narrow;  // narrow: attn_narrow.h, row tiles of 64
     float *part, *ml;  // partial results of the key slices: [split][heads][q_rows][D], [..][2]
 };
@@ -35,17 +35,28 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
     const fo_attn& a = x.a;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 31, lh = lane >> 5;
     const int wq = w % WQ, wk = w / WQ;
-    const int D = a.head_dim, G = a.heads / a.kv_heads;
+    const int D = a.head_dim, G = f.group;
 
-    // workgroup -> (row tile, longest first), sequence, head (or key head and part of its group), key slice
-    int id = blockIdx.x;
-    const int split = id % f.splits;
-    id /= f.splits;
-    const int units = f.pack ? a.kv_heads * f.row_tiles : a.heads;
-    const int u = id % units;
-    id /= units;
-    const int b = id % a.batch, rt = f.pack ? u % f.row_tiles : f.row_tiles - 1 - id / a.batch;
-    const int h0 = f.pack ? (u / f.row_tiles) * G + 32 * rt : u, hk = f.pack ? u / f.row_tiles : u / G;
+    // workgroup: x: head (or key head and part of its group) and key slice, y: sequence,
+    // z: row tile, longest first.  (A grid of three dimensions and branches round the
+    // rest: an integer division is some 40 instructions ahead of the first load.)
+    int u = blockIdx.x, split = 0;
+    if (f.splits > 1) {
+        split = u % f.splits;
+        u /= f.splits;
+    }
+    const int b = blockIdx.y;
+    int h0 = u, hk = u, rt = f.row_tiles - 1 - blockIdx.z;
+    if (f.pack) {
+        rt = 0;
+        if (f.row_tiles > 1) {
+            rt = u % f.row_tiles;
+            hk = u / f.row_tiles;
+        }
+        h0 = hk * G + 32 * rt;
+    } else if (G > 1) {
+        hk = u / G;
+    }
     const Span s = span_of(a, b);
     const int i0 = f.pack ? 0 : rt * 32 * WQ;
     if (i0 >= s.nq) return;
@@ -232,11 +243,12 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
 template <class T, int DP>
 fo_status attn_fwd_launch(const AttnArgs& x, const FwdShape& f, hipStream_t s) {
     const fo_attn& a = x.a;
-    const int64_t n = (int64_t)f.row_tiles * (f.pack ? a.kv_heads : a.heads) * a.batch * f.splits;
+    const dim3 n = f.pack ? dim3((unsigned)(f.row_tiles * a.kv_heads * f.splits), a.batch)
+                          : dim3((unsigned)(a.heads * f.splits), a.batch, f.row_tiles);
     const bool cap = a.cap > 0.f;
     const unsigned lds = a.table && !f.pack ? 4 * lut_floats(a) : 0;
     const bool extra = a.table || x.thr;
-#define FO_FWD(WQ, CAP, EXTRA, VEC) attn_fwd_kernel<T, DP, WQ, CAP, EXTRA, VEC><<<(unsigned)n, 256, lds, s>>>(x, f)
+#define FO_FWD(WQ, CAP, EXTRA, VEC) attn_fwd_kernel<T, DP, WQ, CAP, EXTRA, VEC><<<n, 256, lds, s>>>(x, f)
 #define FO_FWD_W(CAP, EXTRA)                                   \
     {                                                          \
         if (!f.vec) {  /* 33 to 64 rows: one tile either way */ \

@@ -64,7 +64,7 @@ small_bwd_kernel(AttnArgs x) {
     T *Ks = smem, *Vs = smem + L::TILE, *Ps = smem, *Qs = smem + L::A, *Gs = Qs + L::TILE;
     const fo_attn& a = x.a;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lr = lane & 31, lh = lane >> 5;
-    const int D = a.head_dim, R = a.radius, h = blockIdx.x % a.heads, b = blockIdx.x / a.heads;
+    const int D = a.head_dim, R = a.radius, h = blockIdx.x, b = blockIdx.y;
     const Span s = span_of(a, b);
     float* hist = EXTRA && a.table ? x.hist + ((int64_t)b * a.heads + h) * (2 * R + 1) : nullptr;
     if (s.nq == 0 || s.nk == 0) {  // nothing meets: zero gradients for the rows there are
@@ -262,7 +262,7 @@ small_bwd_kernel(AttnArgs x) {
 template <class T, int DP>
 fo_status small_bwd_launch(const AttnArgs& x, hipStream_t s) {
     const fo_attn& a = x.a;
-    const unsigned n = (unsigned)(a.heads * a.batch);
+    const dim3 n(a.heads, a.batch);
     const bool cap = a.cap > 0.f, extra = a.table || x.thr, half = a.max_q <= 64 && a.max_k <= 64;
     const unsigned lds = a.table ? 4 * lut_floats(a) * (half ? 3 : 5) : 0;
 #define FO_SMALL(CAP, EXTRA)                                                            \

@@ -136,6 +136,7 @@ constexpr int kNarrowDim = 8;  // the widest head of attn_narrow.h
 
 FwdShape fwd_shape(const fo_attn& a) {
     FwdShape f{};
+    f.group = a.heads / a.kv_heads;
     f.pack = a.max_q == 1;
     f.narrow = a.head_dim <= kNarrowDim && a.max_q > 32;
     f.wq = f.pack || a.max_q <= 32 ? 1 : a.max_q <= 64 ? 2 : 4;
@@ -150,6 +151,7 @@ FwdShape fwd_shape(const fo_attn& a) {
 
 BwdShape bwd_shape(const fo_attn& a) {
     BwdShape f{};
+    f.group = a.heads / a.kv_heads;
     f.narrow = a.head_dim <= kNarrowDim && a.max_q > 32 && a.max_k > 32;
     if (f.narrow) f.wq = f.wk = kNarrowRows / 32;
     else f.wq = a.max_q <= 32 ? 1 : a.max_q <= 64 ? 2 : 4;
