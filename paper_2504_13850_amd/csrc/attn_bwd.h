@@ -34,13 +34,13 @@ constexpr int bwd_occ() { return sizeof(T) == 4 || DP == 128 ? 1 : 2; }
 
 constexpr int bwd_kb(int wn) { return wn == 4 ? 64 : 32 * (4 / wn); }
 
-// Scores S -> u log2(e) + add, and du/ds.
-template <class T, bool CAP>
-__device__ __forceinline__ void to_exponent(f32x16& S, float* slope, const ScoreK& k, float add) {
+// Scores S -> u log2(e) + add(r), and du/ds.
+template <class T, bool CAP, class F>
+__device__ __forceinline__ void to_exponent(f32x16& S, float* slope, const ScoreK& k, F add) {
     if (CAP) cap_scores<T, 16>(S, k, slope);
-    const float mul = CAP ? 1.f : k.mul;
+    const float mul = CAP ? k.cl : k.mul;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) S[r] = fmaf(S[r], mul, add);
+    for (int r = 0; r < 16; ++r) S[r] = fmaf(S[r], mul, add(r));
 }
 template <class F>
 __device__ __forceinline__ void near_bias(f32x16& S, F f) {
@@ -124,6 +124,9 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
 #pragma unroll
         for (int r = 0; r < 16; ++r) dQ[d][r] = X[d][r] = 0.f;
     float err = 0.f;  // this lane's part of the row sum of dU
+    f32x16 g0;        // dP - delta starts from -delta, unless dropout comes between the two
+#pragma unroll
+    for (int r = 0; r < 16; ++r) g0[r] = EXTRA && x.thr ? 0.f : -dl;
 
     for (int t = 0; t < tiles; ++t) {
         __syncthreads();
@@ -138,9 +141,9 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
         for (int c = 0; c < KT; ++c) {
             const int kw = 32 * (KT * wk + c), j0 = t * KB + kw;
             if (j0 >= wave_end) continue;
-            f32x16 S, G;
+            f32x16 S, G = g0;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) S[r] = G[r] = 0.f;
+            for (int r = 0; r < 16; ++r) S[r] = 0.f;
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
                 S = mma(TL::frag_row(Ks, kw, 16 * kk, lane), q[kk], S);
@@ -150,7 +153,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
             const int n_lo = j0 - (iw + 31) - off, n_hi = j0 + 31 - iw - off;
             const bool near = EXTRA && bias && n_lo < a.radius && n_hi > -a.radius;
             const float add0 = !bias || near ? 0.f : n_lo >= a.radius ? far_hi : far_lo;
-            to_exponent<T, CAP>(S, slope, sc, add0 - lse);
+            const float add = add0 - lse;
+            to_exponent<T, CAP>(S, slope, sc, [&](int) { return add; });
             if (near) {
                 const float* at = &lut[j0 + 4 * lh - qi - off + a.radius + kReach];
                 near_bias(S, [&](int r) { return at[8 * (r >> 2) + (r & 3)]; });
@@ -164,12 +168,12 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
             if (EXTRA && x.thr) {
                 const uint32_t bits = keep_bits(x.thr, j0, lh, qi, b * a.heads + h, a);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) G[r] = (bits >> r) & 1 ? G[r] * x.keep_scale : 0.f;
+                for (int r = 0; r < 16; ++r) G[r] = ((bits >> r) & 1 ? G[r] * x.keep_scale : 0.f) - dl;
             }
             float ds[16], ps[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(S[r]), du = p * (G[r] - dl);
+                const float p = __builtin_amdgcn_exp2f(S[r]), du = p * G[r];
                 err += du;
                 ds[r] = CAP ? du * slope[r] : du;
                 ps[r] = CAP ? p * slope[r] : p;
@@ -345,9 +349,9 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
             sg.load(gb, a.out_ld, t * QB, s.nq, D, tid);
             if (tid < QB) {
                 const int i = t * QB + tid;
-                pl = i < s.nq ? x.lse[stat + i] : INFINITY;  // no such row: P = exp2(-inf) = 0
-                pd = i < s.nq ? x.delta[stat + i] : 0.f;
-                if (pl == -INFINITY) pl = INFINITY;
+                pl = i < s.nq ? -x.lse[stat + i] : -INFINITY;  // no such row: P = exp2(-inf) = 0
+                pd = i < s.nq ? -x.delta[stat + i] : 0.f;
+                if (pl == INFINITY) pl = -INFINITY;
             }
         };
         if (t0 < t1) load(t0);
@@ -358,13 +362,19 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
             if (tid < QB) sl[tid] = pl, sd[tid] = pd;
             __syncthreads();
             if (t + 1 < t1) load(t + 1);
-#pragma unroll 1
+#pragma unroll
             for (int c = 0; c < QT; ++c) {
                 const int qw = 32 * (QT * wk + c), it = t * QB + qw;
                 if (it + 32 <= wave_from || it >= s.nq) continue;
-                f32x16 S, Gd;
+                f32x16 S, Gd;  // sd: -delta, from where dP - delta starts, unless dropout comes between the two
 #pragma unroll
-                for (int r = 0; r < 16; ++r) S[r] = Gd[r] = 0.f;
+                for (int r = 0; r < 16; ++r) S[r] = 0.f;
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    const f32x4 dl = *reinterpret_cast<const f32x4*>(&sd[qw + 8 * q4 + 4 * lh]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) Gd[4 * q4 + e] = EXTRA && x.thr ? 0.f : dl[e];
+                }
 #pragma unroll
                 for (int kk = 0; kk < NK; ++kk) {
                     S = mma(TL::frag_row(Qs, qw, 16 * kk, lane), k[kk], S);
@@ -374,16 +384,13 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
                 const bool near = EXTRA && bias && n0 - 31 < R && n0 + 31 > -R, high = n0 - 31 >= R;
                 const float add0 = !bias || near ? 0.f : high ? far_hi : far_lo;
                 float slope[16];
-                to_exponent<T, CAP>(S, slope, sc, add0);
+                f32x4 ls[4];  // sl: -lse
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) ls[q4] = *reinterpret_cast<const f32x4*>(&sl[qw + 8 * q4 + 4 * lh]);
+                to_exponent<T, CAP>(S, slope, sc, [&](int r) { return EXTRA ? ls[r >> 2][r & 3] + add0 : ls[r >> 2][r & 3]; });
                 if (near) {
                     const float* at = &lut[n0 + lr - 4 * lh + R + kReach];
                     near_bias(S, [&](int r) { return at[-8 * (r >> 2) - (r & 3)]; });
-                }
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 ls = *reinterpret_cast<const f32x4*>(&sl[qw + 8 * q4 + 4 * lh]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) S[4 * q4 + e] -= ls[e];
                 }
                 if (it < wave_all) {
                     const int from = first - it - 4 * lh;
@@ -407,7 +414,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const bool kept = ((e < 2 ? words.x : words.y) >> (kr + 16 * (e & 1))) & 1;
-                            Gd[4 * q4 + e] = kept ? Gd[4 * q4 + e] * x.keep_scale : 0.f;
+                            Gd[4 * q4 + e] = (kept ? Gd[4 * q4 + e] * x.keep_scale : 0.f) + sd[qw + 8 * q4 + 4 * lh + e];
                             ps[4 * q4 + e] = kept ? ps[4 * q4 + e] : 0.f;
                         }
                     }
@@ -420,11 +427,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
                     for (int d = 0; d < ND; ++d) dV[d] = mma(TL::frag_col(Gs, qw + 16 * k2, 32 * d, lane), pf, dV[d]);
                 }
 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 dl = *reinterpret_cast<const f32x4*>(&sd[qw + 8 * q4 + 4 * lh]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) S[4 * q4 + e] *= Gd[4 * q4 + e] - dl[e];  // dU
-                }
+                for (int r = 0; r < 16; ++r) S[r] *= Gd[r];  // dU
                 if (EXTRA && bias) {
                     if (near) {
                         add_diagonals(S, &line[n0 + R + kReach], lr, lh);

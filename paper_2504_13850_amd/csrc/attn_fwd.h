@@ -133,7 +133,7 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
         if (CAP) {
 #pragma unroll
             for (int c = 0; c < KT; ++c) cap_scores<T, 16>(S[c], sc, nullptr);
-            mul = 1.f;
+            mul = sc.cl;
         }
         if (near) {  // x itself takes S's place
             const int base = j0 + 4 * lh - qi - off;

@@ -36,7 +36,7 @@ template <class T, bool CAP, int N>
 __device__ __forceinline__ void narrow_exponent(float (&S)[N], float* slope, const ScoreK& k, float mul, float add) {
     if (CAP) cap_scores<T, N>(S, k, slope);
 #pragma unroll
-    for (int r = 0; r < N; ++r) S[r] = fmaf(S[r], CAP ? 1.f : mul, add);
+    for (int r = 0; r < N; ++r) S[r] = fmaf(S[r], CAP ? k.cl : mul, add);
 }
 
 // Rows of one wave: 64 queries of head h (fwd, dq) or 64 keys of head hk.

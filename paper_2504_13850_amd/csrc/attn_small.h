@@ -132,7 +132,8 @@ small_bwd_kernel(AttnArgs x) {
             const int n_lo = j0 - (iw + 31) - off, n_hi = j0 + 31 - iw - off;
             const bool near = EXTRA && bias && n_lo < R && n_hi > -R;
             const float add0 = !bias || near ? 0.f : n_lo >= R ? far_hi : far_lo;
-            to_exponent<T, CAP>(S[c], slope[c], sc, add0 - lse);
+            const float add = add0 - lse;
+            to_exponent<T, CAP>(S[c], slope[c], sc, [&](int) { return add; });
             if (near) {
                 const float* at = &lut[j0 + 4 * lh - qi - off + R + kReach];
                 near_bias(S[c], [&](int r) { return at[8 * (r >> 2) + (r & 3)]; });

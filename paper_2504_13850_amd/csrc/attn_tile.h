@@ -237,7 +237,7 @@ __device__ __forceinline__ void negate(Frag<T>& f) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f.v[e] = -f.v[e];
 }
-// Scores -> capped scores without their bias, slope = du / ds (or NULL).  A wave
+// Scores -> tanh(cs S), slope = du / ds (or NULL).  A wave
 // whose arguments all stay below 0.35, as scores usually do under their cap, takes
 // the series alone: 9 instructions (fp32) against 16 with two at quarter rate.
 template <class T, int N, class V>
@@ -256,7 +256,7 @@ __device__ __forceinline__ void cap_scores(V& S, const ScoreK& k, float* slope) 
     };
     auto put = [&](int r, float t) {
         if (slope) slope[r] = fmaf(-t, t, 1.f);
-        S[r] = t * k.cl;
+        S[r] = t;
     };
     if (!high) {
 #pragma unroll
