@@ -130,8 +130,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dq_kernel(AttnAr
 
     for (int t = 0; t < tiles; ++t) {
         __syncthreads();
-        sk.store(Ks, tid);
-        sv.store(Vs, tid);
+        sk.store(Ks, tid, D);
+        sv.store(Vs, tid, D);
         __syncthreads();
         if (t + 1 < tiles) {
             sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, tid);
@@ -357,8 +357,8 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
         if (t0 < t1) load(t0);
         for (int t = t0; t < t1; ++t) {
             __syncthreads();
-            sq.store(Qs, tid);
-            sg.store(Gs, tid);
+            sq.store(Qs, tid, D);
+            sg.store(Gs, tid, D);
             if (tid < QB) sl[tid] = pl, sd[tid] = pd;
             __syncthreads();
             if (t + 1 < t1) load(t + 1);

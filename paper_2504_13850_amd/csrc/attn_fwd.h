@@ -108,8 +108,8 @@ attn_fwd_kernel(AttnArgs x, FwdShape f) {
     for (int t = t0; t < t1; ++t) {
         T *Ks = (T*)smem + (BUF == 2 ? (t & 1) * 2 * TILE : 0), *Vs = Ks + TILE;
         if (BUF == 1) __syncthreads();  // the previous tile has been read
-        sk.store(Ks, tid);
-        sv.store(Vs, tid);
+        sk.store(Ks, tid, D);
+        sv.store(Vs, tid, D);
         __syncthreads();
         if (t + 1 < t1) {
             sk.load(kb, a.k_ld, (t + 1) * KB, s.nk, D, tid);

@@ -98,10 +98,10 @@ small_bwd_kernel(AttnArgs x) {
         sg.load((const T*)x.dout + (int64_t)s.q0 * a.out_ld + h * a.out_hs, a.out_ld, 0, s.nq, D, tid);
         sq.clear_past(D, tid);
         sg.clear_past(D, tid);
-        sk.store(Ks, tid);
-        sv.store(Vs, tid);
-        sq.store(Qs, tid);
-        sg.store(Gs, tid);
+        sk.store(Ks, tid, D);
+        sv.store(Vs, tid, D);
+        sq.store(Qs, tid, D);
+        sg.store(Gs, tid, D);
     }
     float lse = ok ? x.lse[stat] : INFINITY, far_lo = 0.f, far_hi = 0.f, sum_lo = 0.f, sum_hi = 0.f;
     if (lse == -INFINITY) lse = INFINITY;
