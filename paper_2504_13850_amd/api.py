@@ -557,7 +557,7 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
     if k_dim != dim or v.shape != k_shape or out.shape != shape:
         raise FoError(FO_EINVAL, f"fo_attn: q {tuple(shape)}, k {tuple(k_shape)}, v {tuple(v.shape)}, "
                                  f"out {tuple(out.shape)}")
-    (ql, qh, q1), (kl, kh, k1), (vl, vh, v1), (ol, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    strides = (ql, qh, q1), (kl, kh, k1), (vl, vh, v1), (ol, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     if k.dtype != ty or v.dtype != ty or out.dtype != ty or (dim > 1 and (q1 != 1 or k1 != 1 or v1 != 1 or o1 != 1)):
         raise FoError(FO_EINVAL, "fo_attn: operands of one type with a contiguous last dimension")
     for t in (q_begin, q_end, k_begin, k_end) if prefix is None else (q_begin, q_end, k_begin, k_end, prefix):
@@ -571,10 +571,30 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
             raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the int32 buckets of 2 radius + 1 "
                                      "distances")
         n_buckets, radius, table_at, bucket_at = table.shape[0], bucket.numel() // 2, table.data_ptr(), bucket.data_ptr()
-    return fo_attn.from_buffer_copy(_ATTN.pack(
+    a = fo_attn.from_buffer_copy(_ATTN.pack(
         dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(), q_end.data_ptr(),
         k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh, dim ** -0.5 if scale is None else scale,
         cap, mask, 0 if prefix is None else prefix.data_ptr(), table_at, bucket_at, n_buckets, radius, p, seed, offset))
+    a.like = ty, (shape, k_shape, k_shape, shape), strides
+    return a
+
+
+def _other_strides(shape, s, t) -> bool:
+    return s != t and any(n > 1 and x != y for n, x, y in zip(shape, s, t))
+
+
+def _fits(attn, q, k, v, out, lse):
+    """The operands have the type, shapes and strides of those that the record was made of."""
+    like = getattr(attn, "like", None)  # (a record filled by hand has none)
+    if like is None:
+        return
+    ty, shapes, strides = like
+    for x, n, s in zip((q, k, v, out), shapes, strides):
+        if x.dtype != ty or x.shape != n or _other_strides(n, x.stride(), s):
+            raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape or strides than the record's")
+    shape = shapes[0]
+    if lse is not None and (lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
+        raise FoError(FO_EINVAL, "fo_attn: lse is fp32 [heads, rows]")
 
 
 def _bytes(ws) -> int:
@@ -590,16 +610,17 @@ def fo_attn_workspace(attn: fo_attn, backward: bool = False) -> int:
 
 
 def fo_attn_fwd(attn: fo_attn, q, k, v, out, lse=None, workspace=None, stream=None):
+    _fits(attn, q, k, v, out, lse)
     _check(lib().fo_attn_fwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
                              _dptr(workspace), _bytes(workspace), _stream(stream)))
 
 
 def fo_attn_bwd(attn: fo_attn, q, k, v, out, lse, dout, dq, dk, dv, dtable=None, workspace=None, stream=None):
     """dout has out's strides; dq, dk and dv have those of q, k and v."""
+    _fits(attn, q, k, v, out, lse)
     ty = q.dtype
     for a, b in ((out, dout), (q, dq), (k, dk), (v, dv)):
-        if b.dtype != ty or a.shape != b.shape or (a.stride() != b.stride() and any(
-                n > 1 and x != y for n, x, y in zip(a.shape, a.stride(), b.stride()))):
+        if b.dtype != ty or a.shape != b.shape or _other_strides(a.shape, a.stride(), b.stride()):
             raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes and strides of what they belong to")
     if dtable is not None and (dtable.dtype != ty or not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
         raise FoError(FO_EINVAL, "fo_attn_bwd: dtable has the table's shape")
