@@ -87,9 +87,11 @@ FO_API int64_t fo_attn_workspace(const fo_attn* a, int32_t backward);
 
 /* Forward.  lse (device fp32 [heads][q_rows], may be NULL) receives the base-2
  * logarithm of sum_j exp(u_ij), -infinity for a query that sees no key: the
- * backward pass needs it.  Keys that no query of their own sequence sees, and rows past a
- * sequence's end, may hold anything; a key that some query of its sequence sees
- * has to be finite.  Errors: FO_EINVAL, FO_EHIP. */
+ * backward pass needs it.  Rows of no sequence may hold anything, and so may the
+ * rows of a cache past a sequence's end.  The rows of a sequence have to be
+ * finite, those that the mask or the bias hides too: a probability of zero still
+ * multiplies its value row, as in a product of matrices.  Errors: FO_EINVAL,
+ * FO_EHIP. */
 FO_API fo_status fo_attn_fwd(const fo_attn* a, const void* q, const void* k, const void* v, void* out, float* lse,
                              void* workspace, int64_t workspace_bytes, void* hip_stream);
 
