@@ -583,50 +583,60 @@ def _other_strides(shape, s, t) -> bool:
     return s != t and any(n > 1 and x != y for n, x, y in zip(shape, s, t))
 
 
-def _fits(attn, q, k, v, out, lse):
-    """The operands have the type, shapes and strides of those that the record was made of."""
-    like = getattr(attn, "like", None)  # (a record filled by hand has none)
-    if like is None:
-        return
+def _fits(like, q, k, v, out) -> bool:
+    """Operands, or their gradients, of the type, shapes and strides that a record was made of."""
     ty, shapes, strides = like
-    for x, n, s in zip((q, k, v, out), shapes, strides):
-        if x.dtype != ty or x.shape != n or _other_strides(n, x.stride(), s):
-            raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape or strides than the record's")
-    shape = shapes[0]
-    if lse is not None and (lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous()):
-        raise FoError(FO_EINVAL, "fo_attn: lse is fp32 [heads, rows]")
+    at = q.stride(), k.stride(), v.stride(), out.stride()
+    return (q.dtype == ty and k.dtype == ty and v.dtype == ty and out.dtype == ty
+            and (q.shape, k.shape, v.shape, out.shape) == shapes
+            and (at == strides or not any(map(_other_strides, shapes, at, strides))))
+
+
+def _check_operands(attn, q, k, v, out, lse):
+    like = getattr(attn, "like", None)
+    if like is None:  # a record filled by hand
+        like = q.dtype, (q.shape, k.shape, v.shape, out.shape), (q.stride(), k.stride(), v.stride(), out.stride())
+    elif not _fits(like, q, k, v, out):
+        raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape or strides than the record's")
+    if lse is not None:
+        shape = like[1][0]
+        if lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous():
+            raise FoError(FO_EINVAL, "fo_attn: lse is fp32 [heads, rows]")
+    return like
 
 
 def _bytes(ws) -> int:
-    return 0 if ws is None else ws.numel() * ws.element_size()
+    return 0 if ws is None else ws.nbytes
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def fo_attn_workspace(attn: fo_attn, backward: bool = False) -> int:
     """Bytes of workspace for fo_attn_fwd, or for both calls."""
-    n = lib().fo_attn_workspace(C.byref(attn), 1 if backward else 0)
+    n = (_lib or lib()).fo_attn_workspace(C.byref(attn), 1 if backward else 0)
     if n < 0:
         raise FoError(FO_EINVAL, last_error())
     return n
 
 
 def fo_attn_fwd(attn: fo_attn, q, k, v, out, lse=None, workspace=None, stream=None):
-    _fits(attn, q, k, v, out, lse)
-    _check(lib().fo_attn_fwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
-                             _dptr(workspace), _bytes(workspace), _stream(stream)))
+    _check_operands(attn, q, k, v, out, lse)
+    _check((_lib or lib()).fo_attn_fwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _addr(lse),
+                             _addr(workspace), _bytes(workspace), _stream(stream)))
 
 
 def fo_attn_bwd(attn: fo_attn, q, k, v, out, lse, dout, dq, dk, dv, dtable=None, workspace=None, stream=None):
     """dout has out's strides; dq, dk and dv have those of q, k and v."""
-    _fits(attn, q, k, v, out, lse)
-    ty = q.dtype
-    for a, b in ((out, dout), (q, dq), (k, dk), (v, dv)):
-        if b.dtype != ty or a.shape != b.shape or _other_strides(a.shape, a.stride(), b.stride()):
-            raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes and strides of what they belong to")
-    if dtable is not None and (dtable.dtype != ty or not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
+    like = _check_operands(attn, q, k, v, out, lse)
+    if not _fits(like, dq, dk, dv, dout):
+        raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes and strides of what they belong to")
+    if dtable is not None and (dtable.dtype != q.dtype or not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
         raise FoError(FO_EINVAL, "fo_attn_bwd: dtable has the table's shape")
-    _check(lib().fo_attn_bwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _dptr(lse),
-                             dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _dptr(dtable),
-                             _dptr(workspace), _bytes(workspace), _stream(stream)))
+    _check((_lib or lib()).fo_attn_bwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _addr(lse),
+                             dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _addr(dtable),
+                             _addr(workspace), _bytes(workspace), _stream(stream)))
 
 
 def fo_relpos_buckets(n_buckets: int, radius: int, causal: bool = False) -> np.ndarray:
