@@ -8,6 +8,10 @@
 // Two passes over the scores, so that every sum has one owner and a fixed order:
 // the query kernel (dq and delta), then the key kernel (dk, dv and the bias
 // sums).  Each recomputes P from the forward pass's lse.
+//
+// Bound by the matrix pipe, which one wave a SIMD (some 400 registers at width 128)
+// does not keep fed: four causal documents of 500 to 4096 tokens, bf16, 16 heads of
+// 128 over 4 key heads, 700 us (640 TFLOP/s over its four products) and 841 us (535).
 #pragma once
 
 #include "attn_tile.h"

@@ -8,8 +8,8 @@
 // wave sums them over the queries for 32 keys.
 //
 // Bound by latency (the chain of loads, five products and five barriers).  The
-// BERT-shaped block, 32 x 12 heads, bias and dropout: the query and the key kernel
-// took 15 and 22 us.
+// BERT-shaped block, 32 x 12 heads, bias and dropout: 25 us; the query and the key
+// kernel took 15 and 22, and a launch more.
 #pragma once
 
 #include "attn_bwd.h"
