@@ -253,7 +253,9 @@ __device__ __forceinline__ void add_diagonals(const f32x16& du, float* line, int
     }
     pos += __shfl_xor(pos, 32);
     neg += __shfl_xor(neg, 32);
+    wave_sync();  // the next tile's 64 distances overlap these by 32, in other lanes
     line[lr - 32 * lh] += lh ? neg : pos;  // 64 lanes, 64 distances
+    wave_sync();
 }
 
 // dk, dv and the bias gradient by distance.  WN waves take 32 keys each, 4 / WN

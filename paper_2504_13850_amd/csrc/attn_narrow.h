@@ -14,12 +14,6 @@
 
 namespace fo {
 
-// Orders a wave's own LDS accesses (the hardware does; this is for the compiler).
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 template <class T, int DN>
 __device__ __forceinline__ void ld_narrow(float* v, const T* row, int D, bool ok) {
 #pragma unroll

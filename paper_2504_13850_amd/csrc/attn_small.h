@@ -37,7 +37,9 @@ __device__ __forceinline__ void add_diagonals_t(const f32x16& du, float* line, i
     }
     pos += __shfl_xor(pos, 32);
     neg += __shfl_xor(neg, 32);
+    wave_sync();  // as in add_diagonals
     line[lr - 32 * lh] += lh ? neg : pos;
+    wave_sync();
 }
 
 // A 16-entry half (registers 8 k2 ..) of a lane's row of a [rows][LM] tile: two runs of four columns.

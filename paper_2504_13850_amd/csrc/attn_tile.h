@@ -24,6 +24,14 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
+// Orders LDS accesses of a wave's lanes that read what another lane has written (the
+// hardware keeps a wave's order; the compiler only a lane's own).
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // An operand of one step of 16 k values: lane l holds row l % 32 and k = 8 (l / 32) + e, e = 0..7.
 template <class T>
 struct Frag;
