@@ -410,13 +410,12 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
                 if (EXTRA && x.thr) {
                     // drawn with the queries on the lanes, as in the other passes, and turned through LDS
                     drops[w][32 * lh + lr] = (uint16_t)keep_bits(x.thr, jw, lh, it + lr, b * a.heads + h, a);
-                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                    wave_sync();
                     const int kr = ((lr >> 3) << 2) | (lr & 3);  // the key's bit in a query's word
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4) {
-                        const uint2 words = *reinterpret_cast<const uint2*>(&drops[w][32 * ((lr >> 2) & 1) + 8 * q4 + 4 * lh]);
+                        uint2 words;
+                        __builtin_memcpy(&words, __builtin_assume_aligned(&drops[w][32 * ((lr >> 2) & 1) + 8 * q4 + 4 * lh], 8), 8);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const bool kept = ((e < 2 ? words.x : words.y) >> (kr + 16 * (e & 1))) & 1;
@@ -424,7 +423,7 @@ __global__ void __launch_bounds__(256, (bwd_occ<T, DP>())) attn_dkv_kernel(AttnA
                             ps[4 * q4 + e] = kept ? ps[4 * q4 + e] : 0.f;
                         }
                     }
-                    __builtin_amdgcn_wave_barrier();  // read before the next tile's words are written
+                    wave_sync();  // read before the next tile's words are written
                 }
 #pragma unroll
                 for (int k2 = 0; k2 < 2; ++k2) {

@@ -21,3 +21,15 @@ def test_bias_gradient_of_every_distance(dtype, lens, heads, kv, dim):
     c.bucket.copy_(torch.arange(2 * radius + 1))
     c.run()
     c.verify()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,heads,kv,dim,radius", [
+    (((300, 300), (129, 257)), 4, 2, 64, None), (((260, 300),), 2, 1, 128, 30), (((700, 40), (33, 31)), 2, 1, 32, None)])
+def test_dropped_probabilities_tile_after_tile(dtype, lens, heads, kv, dim, radius):
+    """The key kernel turns each tile's keep bits through the same words of LDS, one tile right after the other: half of
+    the probabilities dropped, so that bits of a neighbouring tile would show in every gradient."""
+    announce(f"dropout tile after tile {dtype} {lens} {heads} {kv} {dim} {radius}")
+    c = Case(dtype=dtype, lens=lens, heads=heads, kv_heads=kv, dim=dim, radius=radius, p=0.5, seed=61)
+    c.run()
+    c.verify()
