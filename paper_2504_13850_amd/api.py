@@ -533,11 +533,27 @@ def _dtype(t) -> int:
 
 
 def _same(what, ref, *tensors):
-    """The given tensors (None apart) have ref's type, and their last dimension is contiguous."""
-    dt = ref.dtype
+    """The given tensors (None apart) have ref's type and device, and their last dimension is contiguous."""
+    dt, dev = ref.dtype, ref.get_device()
     for t in tensors:
-        if t is not None and (t.dtype != dt or (t.stride(-1) != 1 and t.shape[-1] > 1)):
-            raise FoError(FO_EINVAL, f"{what}: operands of one type with a contiguous last dimension")
+        if t is not None and (t.dtype != dt or t.get_device() != dev or (t.stride(-1) != 1 and t.shape[-1] > 1)):
+            raise FoError(FO_EINVAL, f"{what}: operands of one type on one device with a contiguous last dimension")
+
+
+def _on_gpu(what, dev: int, stream, *tensors):
+    """The call runs on GPU dev (negative: no GPU), and so do its stream and the given tensors (None apart)."""
+    if dev < 0:
+        raise FoError(FO_EINVAL, f"{what}: operands in the GPU's memory")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise FoError(FO_EINVAL, f"{what}: an operand, result or workspace on another device than the others")
+    if stream is None:  # the current device's default stream
+        import torch
+        at = torch.cuda.current_device()
+    else:
+        at = dev if isinstance(stream, int) else stream.device_index
+    if at != dev:
+        raise FoError(FO_EINVAL, f"{what}: a stream of device {at}, operands on device {dev}")
 
 
 # fo_attn as one packed record: building it field by field takes several times as long
@@ -549,8 +565,9 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
               mask: int = FO_ATTN_FULL, prefix=None, table=None, bucket=None, p: float = 0.0, seed: int = 0,
               offset: int = 0) -> fo_attn:
     """The record of an attention over q [rows, heads, dim], k and v [rows, kv_heads, dim] and out like q, whose
-    rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  The record holds addresses: the bounds,
-    prefix, table and bucket tensors have to live until the calls that use it have run."""
+    rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  All tensors are on one device, the GPU of the
+    calls that use the record.  The record holds addresses: the bounds, prefix, table and bucket tensors have to live
+    until those calls have run."""
     dt, ty, batch, i32 = _dtype(q), q.dtype, q_begin.numel(), _INT32[0]
     rows, heads, dim = shape = q.shape
     k_rows, kv_heads, k_dim = k_shape = k.shape
@@ -560,6 +577,10 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
     strides = (ql, qh, q1), (kl, kh, k1), (vl, vh, v1), (ol, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     if k.dtype != ty or v.dtype != ty or out.dtype != ty or (dim > 1 and (q1 != 1 or k1 != 1 or v1 != 1 or o1 != 1)):
         raise FoError(FO_EINVAL, "fo_attn: operands of one type with a contiguous last dimension")
+    dev = q.get_device()
+    for t in (k, v, out, q_begin, q_end, k_begin, k_end, prefix, table, bucket):
+        if t is not None and t.get_device() != dev:
+            raise FoError(FO_EINVAL, "fo_attn: operands, sequence bounds, prefix, table and buckets on one device")
     for t in (q_begin, q_end, k_begin, k_end) if prefix is None else (q_begin, q_end, k_begin, k_end, prefix):
         if t.dtype != i32 or t.numel() != batch or not t.is_contiguous():
             raise FoError(FO_EINVAL, "fo_attn: sequence bounds and prefix are int32, one for each sequence")
@@ -575,7 +596,7 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
         dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(), q_end.data_ptr(),
         k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh, dim ** -0.5 if scale is None else scale,
         cap, mask, 0 if prefix is None else prefix.data_ptr(), table_at, bucket_at, n_buckets, radius, p, seed, offset))
-    a.like = ty, (shape, k_shape, k_shape, shape), strides
+    a.like = ty, (shape, k_shape, k_shape, shape), strides, dev
     return a
 
 
@@ -584,10 +605,11 @@ def _other_strides(shape, s, t) -> bool:
 
 
 def _fits(like, q, k, v, out) -> bool:
-    """Operands, or their gradients, of the type, shapes and strides that a record was made of."""
-    ty, shapes, strides = like
+    """Operands, or their gradients, of the type, shapes, strides and device that a record was made of."""
+    ty, shapes, strides, dev = like
     at = q.stride(), k.stride(), v.stride(), out.stride()
     return (q.dtype == ty and k.dtype == ty and v.dtype == ty and out.dtype == ty
+            and q.get_device() == k.get_device() == v.get_device() == out.get_device() == dev
             and (q.shape, k.shape, v.shape, out.shape) == shapes
             and (at == strides or not any(map(_other_strides, shapes, at, strides))))
 
@@ -595,9 +617,10 @@ def _fits(like, q, k, v, out) -> bool:
 def _check_operands(attn, q, k, v, out, lse):
     like = getattr(attn, "like", None)
     if like is None:  # a record filled by hand
-        like = q.dtype, (q.shape, k.shape, v.shape, out.shape), (q.stride(), k.stride(), v.stride(), out.stride())
-    elif not _fits(like, q, k, v, out):
-        raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape or strides than the record's")
+        like = (q.dtype, (q.shape, k.shape, v.shape, out.shape), (q.stride(), k.stride(), v.stride(), out.stride()),
+                q.get_device())
+    if not _fits(like, q, k, v, out):
+        raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape, strides or device than the record's")
     if lse is not None:
         shape = like[1][0]
         if lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous():
@@ -622,7 +645,8 @@ def fo_attn_workspace(attn: fo_attn, backward: bool = False) -> int:
 
 
 def fo_attn_fwd(attn: fo_attn, q, k, v, out, lse=None, workspace=None, stream=None):
-    _check_operands(attn, q, k, v, out, lse)
+    like = _check_operands(attn, q, k, v, out, lse)
+    _on_gpu("fo_attn_fwd", like[3], stream, lse, workspace)
     _check((_lib or lib()).fo_attn_fwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _addr(lse),
                              _addr(workspace), _bytes(workspace), _stream(stream)))
 
@@ -631,7 +655,8 @@ def fo_attn_bwd(attn: fo_attn, q, k, v, out, lse, dout, dq, dk, dv, dtable=None,
     """dout has out's strides; dq, dk and dv have those of q, k and v."""
     like = _check_operands(attn, q, k, v, out, lse)
     if not _fits(like, dq, dk, dv, dout):
-        raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes and strides of what they belong to")
+        raise FoError(FO_EINVAL, "fo_attn_bwd: gradients have the types, shapes, strides and device of what they belong to")
+    _on_gpu("fo_attn_bwd", like[3], stream, lse, dtable, workspace)
     if dtable is not None and (dtable.dtype != q.dtype or not dtable.is_contiguous() or dtable.numel() != attn.n_buckets * attn.heads):
         raise FoError(FO_EINVAL, "fo_attn_bwd: dtable has the table's shape")
     _check((_lib or lib()).fo_attn_bwd(C.byref(attn), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _addr(lse),
@@ -653,6 +678,7 @@ def fo_dropout_fwd(x, y, p: float, seed: int, offset: int, bias=None, residual=N
     if y.shape != x.shape or (residual is not None and residual.shape != x.shape) or (
             bias is not None and bias.numel() != cols):
         raise FoError(FO_EINVAL, "fo_dropout_fwd: shapes differ")
+    _on_gpu("fo_dropout_fwd", x.get_device(), stream)
     _check(lib().fo_dropout_fwd(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _dptr(bias), _dptr(residual),
                                 0 if residual is None else _ld(residual), p, seed, offset, y.data_ptr(), _ld(y),
                                 _stream(stream)))
@@ -675,5 +701,6 @@ def fo_dropout_bwd(dy, dx, p: float, seed: int, offset: int, dbias=None, workspa
     rows, cols = dy.shape
     if dx.shape != dy.shape or (dbias is not None and dbias.numel() != cols):
         raise FoError(FO_EINVAL, "fo_dropout_bwd: shapes differ")
+    _on_gpu("fo_dropout_bwd", dy.get_device(), stream, workspace)
     _check(lib().fo_dropout_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), p, seed, offset, dx.data_ptr(),
                                 _ld(dx), _dptr(dbias), _dptr(workspace), _bytes(workspace), _stream(stream)))
