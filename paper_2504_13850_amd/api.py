@@ -517,16 +517,21 @@ def fo_conv2d_bf16_ordered(pass_, Bn, H, W, Ci, Co, k, stride, pad, inp, inp_lo,
 
 
 # ------------------------------------------------------------------ transformer operators
-_DTYPES, _INT32 = {}, []  # torch.dtype -> FO_DT_*; torch.int32 (torch is imported on first use)
+_types = None  # ({torch.dtype: FO_DT_*}, torch.int32): torch is imported on first use
+
+
+def _torch_types():
+    global _types
+    got = _types
+    if got is None:  # one assignment of it all: another thread may be in its first call too
+        import torch
+        got = _types = {torch.bfloat16: FO_DT_BF16, torch.float32: FO_DT_F32}, torch.int32
+    return got
 
 
 def _dtype(t) -> int:
     """FO_DT_* of a tensor."""
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: FO_DT_BF16, torch.float32: FO_DT_F32})
-        _INT32.append(torch.int32)
-    got = _DTYPES.get(t.dtype)
+    got = _torch_types()[0].get(t.dtype)
     if got is None:
         raise FoError(FO_EINVAL, f"bfloat16 or float32 operands, not {t.dtype}")
     return got
@@ -568,7 +573,7 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
     rows and heads may have any strides.  scale: 1 / sqrt(dim) if None.  All tensors are on one device, the GPU of the
     calls that use the record.  The record holds addresses: the bounds, prefix, table and bucket tensors have to live
     until those calls have run."""
-    dt, ty, batch, i32 = _dtype(q), q.dtype, q_begin.numel(), _INT32[0]
+    dt, ty, batch, i32 = _dtype(q), q.dtype, q_begin.numel(), _torch_types()[1]
     rows, heads, dim = shape = q.shape
     k_rows, kv_heads, k_dim = k_shape = k.shape
     if k_dim != dim or v.shape != k_shape or out.shape != shape:
