@@ -517,7 +517,7 @@ def fo_conv2d_bf16_ordered(pass_, Bn, H, W, Ci, Co, k, stride, pad, inp, inp_lo,
 
 
 # ------------------------------------------------------------------ transformer operators
-_types = None  # ({torch.dtype: FO_DT_*}, torch.int32): torch is imported on first use
+_types = None  # ({torch.dtype: FO_DT_*}, torch.int32, torch.float32): torch is imported on first use
 
 
 def _torch_types():
@@ -525,7 +525,7 @@ def _torch_types():
     got = _types
     if got is None:  # one assignment of it all: another thread may be in its first call too
         import torch
-        got = _types = {torch.bfloat16: FO_DT_BF16, torch.float32: FO_DT_F32}, torch.int32
+        got = _types = {torch.bfloat16: FO_DT_BF16, torch.float32: FO_DT_F32}, torch.int32, torch.float32
     return got
 
 
@@ -628,7 +628,7 @@ def _check_operands(attn, q, k, v, out, lse):
         raise FoError(FO_EINVAL, "fo_attn: operands of another type, shape, strides or device than the record's")
     if lse is not None:
         shape = like[1][0]
-        if lse.numel() != shape[0] * shape[1] or lse.element_size() != 4 or not lse.is_contiguous():
+        if lse.numel() != shape[0] * shape[1] or lse.dtype != _torch_types()[2] or not lse.is_contiguous():
             raise FoError(FO_EINVAL, "fo_attn: lse is fp32 [heads, rows]")
     return like
 
