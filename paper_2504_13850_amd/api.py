@@ -634,7 +634,12 @@ def _check_operands(attn, q, k, v, out, lse):
 
 
 def _bytes(ws) -> int:
-    return 0 if ws is None else ws.nbytes
+    """Bytes of a workspace: those in its memory, which an expanded or strided tensor has fewer of than elements."""
+    if ws is None:
+        return 0
+    if not ws.is_contiguous():
+        raise FoError(FO_EINVAL, "a workspace is contiguous")
+    return ws.nbytes
 
 
 def _addr(t):
@@ -681,8 +686,8 @@ def fo_dropout_fwd(x, y, p: float, seed: int, offset: int, bias=None, residual=N
     _same("fo_dropout_fwd", x, x, y, bias, residual)
     rows, cols = x.shape
     if y.shape != x.shape or (residual is not None and residual.shape != x.shape) or (
-            bias is not None and bias.numel() != cols):
-        raise FoError(FO_EINVAL, "fo_dropout_fwd: shapes differ")
+            bias is not None and (bias.numel() != cols or not bias.is_contiguous())):
+        raise FoError(FO_EINVAL, "fo_dropout_fwd: shapes differ, or a bias that is not contiguous")
     _on_gpu("fo_dropout_fwd", x.get_device(), stream)
     _check(lib().fo_dropout_fwd(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _dptr(bias), _dptr(residual),
                                 0 if residual is None else _ld(residual), p, seed, offset, y.data_ptr(), _ld(y),
@@ -704,8 +709,8 @@ def fo_dropout_workspace(rows: int, cols: int) -> int:
 def fo_dropout_bwd(dy, dx, p: float, seed: int, offset: int, dbias=None, workspace=None, stream=None):
     _same("fo_dropout_bwd", dy, dy, dx, dbias)
     rows, cols = dy.shape
-    if dx.shape != dy.shape or (dbias is not None and dbias.numel() != cols):
-        raise FoError(FO_EINVAL, "fo_dropout_bwd: shapes differ")
+    if dx.shape != dy.shape or (dbias is not None and (dbias.numel() != cols or not dbias.is_contiguous())):
+        raise FoError(FO_EINVAL, "fo_dropout_bwd: shapes differ, or a dbias that is not contiguous")
     _on_gpu("fo_dropout_bwd", dy.get_device(), stream, workspace)
     _check(lib().fo_dropout_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), p, seed, offset, dx.data_ptr(),
                                 _ld(dx), _dptr(dbias), _dptr(workspace), _bytes(workspace), _stream(stream)))
