@@ -11,8 +11,10 @@ namespace {
 int64_t elem_size(int32_t dtype) { return dtype == FO_DT_BF16 ? 2 : 4; }
 bool aligned(const void* p, int64_t n) { return ((uintptr_t)p & (uintptr_t)(n - 1)) == 0; }
 
-// A [rows][heads][dim] operand: distinct elements have distinct addresses, and the last offset fits int64.
-fo_status check_strides(const char* what, int64_t rows, int32_t heads, int32_t dim, int64_t ld, int64_t hs) {
+// A [rows][heads][dim] operand of elements of `size` bytes: distinct elements have distinct addresses, and the last
+// one's offset in bytes fits int64.
+fo_status check_strides(const char* what, int64_t rows, int32_t heads, int32_t dim, int64_t ld, int64_t hs,
+                        int64_t size) {
     constexpr int64_t kMaxStride = int64_t(1) << 40;
     FO_CHECK(ld >= 0 && hs >= 0 && ld <= kMaxStride && hs <= kMaxStride, "fo_attn: %s strides %lld, %lld", what,
              (long long)ld, (long long)hs);
@@ -21,6 +23,9 @@ fo_status check_strides(const char* what, int64_t rows, int32_t heads, int32_t d
                              (heads == 1 || (__int128)hs >= (__int128)(rows > 0 ? rows - 1 : 0) * ld + dim);
     FO_CHECK(rows_outer || heads_outer, "fo_attn: %s strides %lld, %lld overlap (%lld rows, %d heads of %d)", what,
              (long long)ld, (long long)hs, (long long)rows, heads, dim);
+    const __int128 last = (__int128)(rows > 0 ? rows - 1 : 0) * ld + (__int128)(heads - 1) * hs + dim;
+    FO_CHECK(last * size <= INT64_MAX, "fo_attn: %s strides %lld, %lld pass 2^63 bytes (%lld rows, %d heads)", what,
+             (long long)ld, (long long)hs, (long long)rows, heads);
     return FO_OK;
 }
 
@@ -40,10 +45,11 @@ fo_status check_attn(const fo_attn* a) {
              "fo_attn: more workgroups than a launch holds");
     FO_CHECK(a->q_begin && a->q_end && a->k_begin && a->k_end, "fo_attn: NULL sequence bounds");
     fo_status st;
-    if ((st = check_strides("q", a->q_rows, a->heads, a->head_dim, a->q_ld, a->q_hs)) != FO_OK) return st;
-    if ((st = check_strides("k", a->k_rows, a->kv_heads, a->head_dim, a->k_ld, a->k_hs)) != FO_OK) return st;
-    if ((st = check_strides("v", a->k_rows, a->kv_heads, a->head_dim, a->v_ld, a->v_hs)) != FO_OK) return st;
-    if ((st = check_strides("out", a->q_rows, a->heads, a->head_dim, a->out_ld, a->out_hs)) != FO_OK) return st;
+    const int64_t e = elem_size(a->dtype);
+    if ((st = check_strides("q", a->q_rows, a->heads, a->head_dim, a->q_ld, a->q_hs, e)) != FO_OK) return st;
+    if ((st = check_strides("k", a->k_rows, a->kv_heads, a->head_dim, a->k_ld, a->k_hs, e)) != FO_OK) return st;
+    if ((st = check_strides("v", a->k_rows, a->kv_heads, a->head_dim, a->v_ld, a->v_hs, e)) != FO_OK) return st;
+    if ((st = check_strides("out", a->q_rows, a->heads, a->head_dim, a->out_ld, a->out_hs, e)) != FO_OK) return st;
     FO_CHECK(std::isfinite(a->scale), "fo_attn: scale is not finite");
     FO_CHECK(std::isfinite(a->cap) && a->cap >= 0.f, "fo_attn: cap=%g", a->cap);
     FO_CHECK(a->mask == FO_ATTN_FULL || a->mask == FO_ATTN_CAUSAL || a->mask == FO_ATTN_PREFIX, "fo_attn: mask=%d",
@@ -149,8 +155,10 @@ static fo_status check_drop(const char* what, int32_t dtype, int64_t rows, int32
     constexpr int64_t kMaxStride = int64_t(1) << 31;
     FO_CHECK(x_ld >= cols && y_ld >= cols && x_ld <= kMaxStride && y_ld <= kMaxStride,
              "%s: row strides %lld, %lld for %d columns", what, (long long)x_ld, (long long)y_ld, cols);
-    FO_CHECK(p >= 0.f && p < 1.f, "%s: p=%g outside [0, 1)", what, p);
     const int64_t e = elem_size(dtype);
+    FO_CHECK((__int128)rows * x_ld * e <= INT64_MAX && (__int128)rows * y_ld * e <= INT64_MAX,
+             "%s: %lld rows of strides %lld, %lld pass 2^63 bytes", what, (long long)rows, (long long)x_ld, (long long)y_ld);
+    FO_CHECK(p >= 0.f && p < 1.f, "%s: p=%g outside [0, 1)", what, p);
     FO_CHECK(aligned(x, e) && aligned(y, e), "%s: unaligned operand", what);
     return FO_OK;
 }
@@ -161,8 +169,8 @@ extern "C" fo_status fo_dropout_fwd(int32_t dtype, int64_t rows, int32_t cols, c
     const fo_status st = check_drop("fo_dropout_fwd", dtype, rows, cols, x, x_ld, y, y_ld, p);
     if (st != FO_OK) return st;
     const int64_t e = elem_size(dtype);
-    FO_CHECK(!residual || (res_ld >= cols && res_ld <= (int64_t(1) << 31)), "fo_dropout_fwd: residual row stride %lld",
-             (long long)res_ld);
+    FO_CHECK(!residual || (res_ld >= cols && res_ld <= (int64_t(1) << 31) && (__int128)rows * res_ld * e <= INT64_MAX),
+             "fo_dropout_fwd: residual row stride %lld", (long long)res_ld);
     FO_CHECK(aligned(bias, e) && aligned(residual, e), "fo_dropout_fwd: unaligned operand");
     if (rows == 0) return FO_OK;
     DropArgs d{};
