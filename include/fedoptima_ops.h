@@ -70,7 +70,9 @@ typedef struct {
     /* Element (row r, head h, d) of x is at x[r x_ld + h x_hs + d], strides in elements. */
     int64_t q_ld, q_hs, k_ld, k_hs, v_ld, v_hs, out_ld, out_hs;
     float scale;                         /* usually 1 / sqrt(head_dim)                         */
-    float cap;                           /* >= 0; 0: scores are not capped                     */
+    float cap;                           /* >= 0; 0: scores are not capped.  scale log2(e),
+                                          * cap log2(e) and scale / cap have to be finite in
+                                          * fp32                                               */
     int32_t mask;                        /* FO_ATTN_*                                          */
     const int32_t* prefix;               /* FO_ATTN_PREFIX: device int32[batch]                */
     const void* table;                   /* bias [n_buckets][heads], or NULL for none          */

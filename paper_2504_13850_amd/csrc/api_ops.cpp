@@ -50,8 +50,11 @@ fo_status check_attn(const fo_attn* a) {
     if ((st = check_strides("k", a->k_rows, a->kv_heads, a->head_dim, a->k_ld, a->k_hs, e)) != FO_OK) return st;
     if ((st = check_strides("v", a->k_rows, a->kv_heads, a->head_dim, a->v_ld, a->v_hs, e)) != FO_OK) return st;
     if ((st = check_strides("out", a->q_rows, a->heads, a->head_dim, a->out_ld, a->out_hs, e)) != FO_OK) return st;
-    FO_CHECK(std::isfinite(a->scale), "fo_attn: scale is not finite");
-    FO_CHECK(std::isfinite(a->cap) && a->cap >= 0.f, "fo_attn: cap=%g", a->cap);
+    // the kernels multiply by scale log2(e), or by scale / cap and cap log2(e), rounded to fp32
+    constexpr float kLog2e = 1.4426950408889634f;
+    FO_CHECK(std::isfinite(a->scale * kLog2e), "fo_attn: scale=%g", a->scale);
+    FO_CHECK(a->cap >= 0.f && std::isfinite(a->cap * kLog2e) && (a->cap == 0.f || std::isfinite(a->scale / a->cap)),
+             "fo_attn: cap=%g, scale=%g", a->cap, a->scale);
     FO_CHECK(a->mask == FO_ATTN_FULL || a->mask == FO_ATTN_CAUSAL || a->mask == FO_ATTN_PREFIX, "fo_attn: mask=%d",
              a->mask);
     FO_CHECK((a->mask == FO_ATTN_PREFIX) == (a->prefix != nullptr), "fo_attn: prefix lengths go with FO_ATTN_PREFIX");

@@ -39,3 +39,17 @@ def test_dropout_offsets_past_64_bits():
         assert L.fo_dropout_fwd(A.FO_DT_F32, MANY, 8, x, xl, None, x, rl, 0.1, 1, 1, x + 64, yl, None) == A.FO_EINVAL
     for xl, yl in ((far, 8), (8, far)):
         assert L.fo_dropout_bwd(A.FO_DT_F32, MANY, 8, x, xl, 0.1, 1, 1, x + 64, yl, None, None, 0, None) == A.FO_EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(cap=3e38), dict(cap=1e-40), dict(scale=3e38), dict(scale=-3e38),
+                                 dict(scale=1e30, cap=1e-10)],
+                         ids=lambda b: ",".join(f"{k}={v}" for k, v in b.items()))
+def test_factors_past_fp32(bad):
+    """scale log2(e), cap log2(e) and scale / cap are the kernels' factors; an infinite one makes every score NaN."""
+    assert _refused(_record(**bad))
+
+
+def test_factors_within_fp32():
+    for good in (dict(cap=1e38), dict(cap=1e-37), dict(scale=2e38), dict(scale=0.0), dict(scale=0.0, cap=1e-40)):
+        a = _record(**good)
+        assert A.lib().fo_attn_workspace(C.byref(a), 1) >= 0, good
