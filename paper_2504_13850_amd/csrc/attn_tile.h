@@ -266,7 +266,7 @@ struct ScoreK {
 };
 __device__ __forceinline__ ScoreK score_k(const fo_attn& a) {
     ScoreK k;
-    k.mul = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);
+    k.mul = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);  // the least normal number
     k.cs = a.cap > 0.f ? a.scale / a.cap : 0.f;
     k.cl = a.cap * kLog2e;
     return k;
