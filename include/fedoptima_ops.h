@@ -129,15 +129,15 @@ FO_API fo_status fo_relpos_buckets(int32_t n_buckets, int32_t radius, int32_t ca
  * (low halves first) of call (n % 2^32, n / 2^32, 0, offset), n = r ceil(cols /
  * 8) + c / 8: the mask depends on rows, columns, seed and offset alone.
  *
- * bias ([cols]) and residual may be NULL; y may be x or residual.  ld: row
- * strides in elements, >= cols.  Errors: FO_EINVAL, FO_EHIP. */
+ * bias ([cols]) and residual may be NULL; y may be x or residual, with its row
+ * stride.  ld: row strides in elements, >= cols.  Errors: FO_EINVAL, FO_EHIP. */
 FO_API fo_status fo_dropout_fwd(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld,
                                 const void* bias, const void* residual, int64_t res_ld, float p, uint64_t seed,
                                 uint32_t offset, void* y, int64_t y_ld, void* hip_stream);
 
 /* dx = drop dy (the residual's gradient is dy itself); dbias ([cols], may be
  * NULL) = the column sums of drop dy before their rounding, and needs the
- * workspace.  dx may be dy. */
+ * workspace.  dx may be dy, with its row stride. */
 FO_API int64_t fo_dropout_workspace(int64_t rows, int32_t cols);
 FO_API fo_status fo_dropout_bwd(int32_t dtype, int64_t rows, int32_t cols, const void* dy, int64_t dy_ld, float p,
                                 uint64_t seed, uint32_t offset, void* dx, int64_t dx_ld, void* dbias,

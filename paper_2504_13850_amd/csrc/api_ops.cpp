@@ -149,6 +149,11 @@ extern "C" fo_status fo_relpos_buckets(int32_t n_buckets, int32_t radius, int32_
     return FO_OK;
 }
 
+// Rows written over rows that are read: element over element, or a thread's rows would be another's.
+static bool in_place(const void* x, int64_t x_ld, const void* y, int64_t y_ld, int64_t rows) {
+    return x != y || rows <= 1 || x_ld == y_ld;
+}
+
 static fo_status check_drop(const char* what, int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld,
                             const void* y, int64_t y_ld, float p) {
     FO_CHECK(dtype == FO_DT_BF16 || dtype == FO_DT_F32, "%s: dtype=%d", what, dtype);
@@ -159,6 +164,8 @@ static fo_status check_drop(const char* what, int32_t dtype, int64_t rows, int32
     FO_CHECK(x_ld >= cols && y_ld >= cols && x_ld <= kMaxStride && y_ld <= kMaxStride,
              "%s: row strides %lld, %lld for %d columns", what, (long long)x_ld, (long long)y_ld, cols);
     const int64_t e = elem_size(dtype);
+    FO_CHECK(in_place(x, x_ld, y, y_ld, rows), "%s: in place with row strides %lld and %lld", what, (long long)x_ld,
+             (long long)y_ld);
     FO_CHECK((__int128)rows * x_ld * e <= INT64_MAX && (__int128)rows * y_ld * e <= INT64_MAX,
              "%s: %lld rows of strides %lld, %lld pass 2^63 bytes", what, (long long)rows, (long long)x_ld, (long long)y_ld);
     FO_CHECK(p >= 0.f && p < 1.f, "%s: p=%g outside [0, 1)", what, p);
@@ -174,6 +181,8 @@ extern "C" fo_status fo_dropout_fwd(int32_t dtype, int64_t rows, int32_t cols, c
     const int64_t e = elem_size(dtype);
     FO_CHECK(!residual || (res_ld >= cols && res_ld <= (int64_t(1) << 31) && (__int128)rows * res_ld * e <= INT64_MAX),
              "fo_dropout_fwd: residual row stride %lld", (long long)res_ld);
+    FO_CHECK(!residual || in_place(residual, res_ld, y, y_ld, rows),
+             "fo_dropout_fwd: in place with row strides %lld and %lld", (long long)res_ld, (long long)y_ld);
     FO_CHECK(aligned(bias, e) && aligned(residual, e), "fo_dropout_fwd: unaligned operand");
     if (rows == 0) return FO_OK;
     DropArgs d{};

@@ -53,3 +53,14 @@ def test_factors_within_fp32():
     for good in (dict(cap=1e38), dict(cap=1e-37), dict(scale=2e38), dict(scale=0.0), dict(scale=0.0, cap=1e-40)):
         a = _record(**good)
         assert A.lib().fo_attn_workspace(C.byref(a), 1) >= 0, good
+
+
+def test_dropout_in_place_with_another_stride():
+    """Rows written over others that are still to be read."""
+    L, x = A.lib(), np.zeros(64, np.int64).ctypes.data
+    fwd = lambda xl, r, rl, y, yl: L.fo_dropout_fwd(  # noqa: E731
+        A.FO_DT_BF16, 3, 8, x, xl, None, r, rl, 0.1, 1, 1, y, yl, None)
+    assert fwd(16, None, 0, x, 8) == A.FO_EINVAL and fwd(8, None, 0, x, 16) == A.FO_EINVAL
+    assert fwd(8, x + 256, 16, x + 256, 8) == A.FO_EINVAL
+    for xl, yl in ((16, 8), (8, 16)):
+        assert L.fo_dropout_bwd(A.FO_DT_BF16, 3, 8, x, xl, 0.1, 1, 1, x, yl, None, None, 0, None) == A.FO_EINVAL
