@@ -564,6 +564,7 @@ def _on_gpu(what, dev: int, stream, *tensors):
 # fo_attn as one packed record: building it field by field takes several times as long
 _ATTN = struct.Struct("@7i2q4P8q2fi3P2ifQI0q")
 assert _ATTN.size == C.sizeof(fo_attn)
+_U64, _U32 = (1 << 64) - 1, (1 << 32) - 1  # seeds and offsets count modulo these, as ctypes passes dropout's
 
 
 def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: int, scale=None, cap: float = 0.0,
@@ -597,10 +598,15 @@ def make_attn(q, k, v, out, q_begin, q_end, k_begin, k_end, max_q: int, max_k: i
             raise FoError(FO_EINVAL, "fo_attn: a contiguous table [buckets, heads] and the int32 buckets of 2 radius + 1 "
                                      "distances")
         n_buckets, radius, table_at, bucket_at = table.shape[0], bucket.numel() // 2, table.data_ptr(), bucket.data_ptr()
-    a = fo_attn.from_buffer_copy(_ATTN.pack(
-        dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(), q_end.data_ptr(),
-        k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh, dim ** -0.5 if scale is None else scale,
-        cap, mask, 0 if prefix is None else prefix.data_ptr(), table_at, bucket_at, n_buckets, radius, p, seed, offset))
+    try:
+        packed = _ATTN.pack(
+            dt, batch, heads, kv_heads, dim, max_q, max_k, rows, k_rows, q_begin.data_ptr(), q_end.data_ptr(),
+            k_begin.data_ptr(), k_end.data_ptr(), ql, qh, kl, kh, vl, vh, ol, oh,
+            dim ** -0.5 if scale is None else scale, cap, mask, 0 if prefix is None else prefix.data_ptr(), table_at,
+            bucket_at, n_buckets, radius, p, seed & _U64, offset & _U32)
+    except struct.error as e:
+        raise FoError(FO_EINVAL, f"fo_attn: an argument outside its type's range ({e})") from None
+    a = fo_attn.from_buffer_copy(packed)
     a.like = ty, (shape, k_shape, k_shape, shape), strides, dev
     return a
 
