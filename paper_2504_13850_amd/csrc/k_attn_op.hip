@@ -188,6 +188,8 @@ BwdShape bwd_shape(const fo_attn& a) {
     // 512 query rows of one head or more, so that the cuts' sums stay a small part.
     const int64_t wgs = std::max<int64_t>(1, (int64_t)f.k_tiles * a.kv_heads * a.batch / (f.narrow ? 4 : 1)), G = a.heads / a.kv_heads;
     const int64_t cuts = std::max<int64_t>(1, std::min<int64_t>({cdiv(512, wgs), G * a.max_q / 512, 64}));
+    f.h_parts = f.q_parts = 1;
+    if (!f.k_tiles) return f;  // no key rows: nothing to cut or to join
     f.h_parts = (int)std::min(G, cuts);
     while (G % f.h_parts) --f.h_parts;
     f.q_parts = (int)(cuts / f.h_parts);
