@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) narrow_fwd(AttnArgs x, FwdShape f) {
     extern __shared__ float lut_all[];
     const fo_attn& a = x.a;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, D = a.head_dim;
-    int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);
+    int id = __builtin_amdgcn_readfirstlane(block_of() * 4 + w);
     const int split = id % f.splits;
     id /= f.splits;
     const int h = id % a.heads, hk = h / (a.heads / a.kv_heads);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256) narrow_dq(AttnArgs x, BwdShape f) {
     extern __shared__ float lut_all[];
     const fo_attn& a = x.a;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, D = a.head_dim;
-    int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);
+    int id = __builtin_amdgcn_readfirstlane(block_of() * 4 + w);
     const int h = id % a.heads, hk = h / (a.heads / a.kv_heads);
     id /= a.heads;
     const int b = id % a.batch, i0 = (f.q_tiles - 1 - id / a.batch) * kNarrowRows;
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(256) narrow_dkv(AttnArgs x, BwdShape f) {
     const fo_attn& a = x.a;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int D = a.head_dim, G = a.heads / a.kv_heads, R = a.radius, W = lut_floats(a);
-    int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);
+    int id = __builtin_amdgcn_readfirstlane(block_of() * 4 + w);
     const int hk = id % a.kv_heads;
     id /= a.kv_heads;
     const int b = id % a.batch;
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(256) narrow_dkv(AttnArgs x, BwdShape f) {
 template <class T, int DN>
 fo_status narrow_fwd_launch(const AttnArgs& x, const FwdShape& f, hipStream_t s) {
     const fo_attn& a = x.a;
-    const unsigned n = (unsigned)cdiv((int64_t)f.row_tiles * a.heads * a.batch * f.splits, 4);
+    const dim3 n = grid_of(cdiv((int64_t)f.row_tiles * a.heads * a.batch * f.splits, 4));
     const unsigned lds = a.table ? 16 * lut_floats(a) : 0;
     const bool cap = a.cap > 0.f, extra = a.table || x.thr;
     if (cap && extra) narrow_fwd<T, DN, true, true><<<n, 256, lds, s>>>(x, f);
@@ -469,7 +469,7 @@ fo_status narrow_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s)
     const unsigned lds = a.table ? 16 * lut_floats(a) : 0;
     const bool cap = a.cap > 0.f, extra = a.table || x.thr;
     if (f.q_tiles) {
-        const unsigned n = (unsigned)cdiv((int64_t)f.q_tiles * a.heads * a.batch, 4);
+        const dim3 n = grid_of(cdiv((int64_t)f.q_tiles * a.heads * a.batch, 4));
         if (cap && extra) narrow_dq<T, DN, true, true><<<n, 256, lds, s>>>(x, f);
         else if (cap) narrow_dq<T, DN, true, false><<<n, 256, lds, s>>>(x, f);
         else if (extra) narrow_dq<T, DN, false, true><<<n, 256, lds, s>>>(x, f);
@@ -477,7 +477,7 @@ fo_status narrow_bwd_launch(const AttnArgs& x, const BwdShape& f, hipStream_t s)
         FO_LAUNCHED();
     }
     if (f.k_tiles) {
-        const unsigned n = (unsigned)cdiv((int64_t)f.k_tiles * f.h_parts * f.q_parts * a.kv_heads * a.batch, 4);
+        const dim3 n = grid_of(cdiv((int64_t)f.k_tiles * f.h_parts * f.q_parts * a.kv_heads * a.batch, 4));
         if (cap && extra) narrow_dkv<T, DN, true, true><<<n, 256, 2 * lds, s>>>(x, f);
         else if (cap) narrow_dkv<T, DN, true, false><<<n, 256, 2 * lds, s>>>(x, f);
         else if (extra) narrow_dkv<T, DN, false, true><<<n, 256, 2 * lds, s>>>(x, f);

@@ -13,6 +13,15 @@ inline uint32_t drop_threshold(float p) {
     return t >= 65535.0 ? 65535u : (uint32_t)t;
 }
 
+// A grid of n workgroups in two dimensions: one dimension holds 2^32 threads, and a launch
+// of more wraps round without an error.  Workgroups past n, in the last row, have no work.
+constexpr int kGridBits = 22;
+inline dim3 grid_of(int64_t n) {
+    return n <= int64_t(1) << kGridBits ? dim3((unsigned)n)
+                                        : dim3(1u << kGridBits, (unsigned)cdiv(n, int64_t(1) << kGridBits));
+}
+__device__ __forceinline__ int block_of() { return (int)((blockIdx.y << kGridBits) + blockIdx.x); }
+
 // Philox 4x32 (Salmon et al., 2011): four words out of four counter words and a
 // two-word key.  Seven rounds, the fewest that the paper finds to pass every
 // TestU01 battery; its usual ten cost 3/7 more of a pass that is bound by its
