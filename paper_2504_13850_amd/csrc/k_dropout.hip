@@ -160,7 +160,7 @@ template <class T>
 __global__ void __launch_bounds__(1024) dbias_kernel(const float* __restrict__ part, int parts, int cols,
                                                     T* __restrict__ out) {
     __shared__ float sums[32][32];
-    const int t = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + t;
+    const int t = threadIdx.x & 31, y = threadIdx.x >> 5, c = block_of() * 32 + t;
     float s = 0.f;
     if (c < cols) {
 #pragma unroll 8
@@ -196,7 +196,7 @@ fo_status bwd(const DropArgs& d, void* dbias, float* ws, hipStream_t s) {
         if (st != FO_OK) return st;
     }
     if (dbias) {
-        dbias_kernel<T><<<(unsigned)cdiv(d.cols, 32), 1024, 0, s>>>(ws, f.parts, d.cols, (T*)dbias);
+        dbias_kernel<T><<<grid_of(cdiv(d.cols, 32)), 1024, 0, s>>>(ws, f.parts, d.cols, (T*)dbias);
         FO_LAUNCHED();
     }
     return FO_OK;

@@ -15,7 +15,7 @@ inline uint32_t drop_threshold(float p) {
 
 // A grid of n workgroups in two dimensions: one dimension holds 2^32 threads, and a launch
 // of more wraps round without an error.  Workgroups past n, in the last row, have no work.
-constexpr int kGridBits = 22;
+constexpr int kGridBits = 20;  // workgroups of up to 1024 threads
 inline dim3 grid_of(int64_t n) {
     return n <= int64_t(1) << kGridBits ? dim3((unsigned)n)
                                         : dim3(1u << kGridBits, (unsigned)cdiv(n, int64_t(1) << kGridBits));
