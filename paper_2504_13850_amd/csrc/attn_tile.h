@@ -256,9 +256,10 @@ __device__ __forceinline__ void store_row(T* row, const f32x16* acc, float s, in
 
 // ------------------------------------------------------------------ scores, base 2
 // u log2(e) = S mul + add, or with a cap cl tanh(cs S) + add.  tanh(y) = 1 - 2 / (e^2y
-// + 1), off by some 2^-23, far below a bf16 probability's rounding; fp32 takes this
-// form above |y| = 0.35 and the series of tanh below, where it would lose the leading
-// digits.
+// + 1), off by up to 2^-21 where y is far below zero and the quotient near 2: far below
+// a bf16 probability's rounding.  fp32 takes |y| there, whose quotient is small (2^-23
+// at 0.35, less above), and below 0.35, where this form would lose the leading digits,
+// the series of tanh.
 struct ScoreK {
     float mul;   // |scale| log2(e), not 0 so that it orders the scores and keeps -infinity
     float cs;    // scale / cap
@@ -305,8 +306,9 @@ __device__ __forceinline__ void cap_scores(V& S, const ScoreK& k, float* slope) 
 #pragma unroll
         for (int r = 0; r < N; ++r) {
             const float y = S[r] * k.cs;
-            float t = fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * kLog2e)) + 1.f), -2.f, 1.f);
-            if (sizeof(T) == 4) t = fabsf(y) < 0.35f ? series(y) : t;
+            const float z = sizeof(T) == 4 ? fabsf(y) : y;
+            float t = fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * (2.f * kLog2e)) + 1.f), -2.f, 1.f);
+            if (sizeof(T) == 4) t = z < 0.35f ? series(y) : copysignf(t, y);
             put(r, t);
         }
     }
