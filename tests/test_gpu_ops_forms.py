@@ -87,3 +87,10 @@ def test_capped_scores_of_several_caps(kw, dtype):
     """Scores whose spread is several caps, so that most of them are held by the cap, and a cap of thousands."""
     check(dtype=dtype, mask=1, cap=50.0, scale=20.0, seed=505, **kw)
     check(dtype=dtype, mask=1, cap=1000.0, scale=0.125, seed=506, **kw)
+
+
+@DTYPES
+@pytest.mark.parametrize("lens,kv", [(((20, 300), (32, 5)), 1), (((130, 40), (64, 64)), 2), (((300, 60),), 1), (((60, 20),), 1)])
+def test_widest_rows_and_radius(dtype, lens, kv):
+    """Heads of 128 and a radius of 1024: the most LDS that each form of the tiled kernels takes."""
+    check(dtype=dtype, lens=lens, heads=2, kv_heads=kv, dim=128, radius=1024, p=0.1, seed=507)
