@@ -15,7 +15,12 @@
  *     contents need not be kept between calls.
  *   - Arguments are checked on the host (FO_EINVAL before any launch).
  *   - dtype names the type of all operands and results of a call; sums, softmax
- *     statistics and the workspace are fp32.
+ *     statistics and the workspace are fp32.  In bf16 the operands of the matrix
+ *     products are bf16 too: probabilities (after dropout) before their products
+ *     with v and dout, score gradients before theirs with q and k are rounded once
+ *     (heads of up to eight columns keep them in fp32).  The tanh of a cap is
+ *     within 2^-19 in bf16 calls, 2^-22 in fp32 calls, so that a score is within
+ *     that times the cap.
  *   - Results do not depend on timing: no sum's order varies between calls.
  */
 #ifndef FEDOPTIMA_OPS_H
@@ -100,6 +105,8 @@ FO_API fo_status fo_attn_fwd(const fo_attn* a, const void* q, const void* k, con
 /* Backward.  q, k, v as in the forward call, out and lse as it left them, dout
  * with out's strides.  dq, dk, dv have the strides of q, k and v; every row of
  * a sequence is written (a shared key head gets the sum over its heads).
+ * The rows of a sequence in out, lse and dout have to be finite as those of q, k
+ * and v (lse apart where it is -infinity).
  * dtable ([n_buckets][heads], may be NULL without a table; else required)
  * receives the table's gradient, 0 for buckets that no visible pair has.
  * Errors: FO_EINVAL, FO_EHIP. */

@@ -11,7 +11,11 @@
 //
 // Bound by the matrix pipe, which one wave a SIMD (some 400 registers at width 128)
 // does not keep fed: four causal documents of 500 to 4096 tokens, bf16, 16 heads of
-// 128 over 4 key heads, 700 us (640 TFLOP/s over its four products) and 841 us (535).
+// 128 over 4 key heads, capped, 700 us (640 TFLOP/s over its four products) and 847 us
+// (530).  EXTRA is one form for a bias, for dropout and for both: the key kernel with it
+// spills 16 to 87 registers in bf16 at width 64 (37 with a bias, four waves over keys and
+// aligned rows: 61 us on six prefix sequences of 700 to 1023 tokens, 12 over 4 heads),
+// and the fp32 one at width 128 up to 90, with a cap 14 and 28 of them without EXTRA too.
 #pragma once
 
 #include "attn_tile.h"

@@ -21,10 +21,13 @@ constexpr int fwd_kb(int wq) { return 32 * fwd_kt(wq) * (4 / wq); }
 // K and V tiles pass through registers into LDS, the next tile's loads in flight
 // during the products.  EXTRA: a bias or dropout.  VEC: see ld_chunk.
 //
-// Long sequences are bound by the matrix pipe beside the exponentials: 13k tokens in
-// two causal documents, bf16, 32 heads of 128 over 8 key heads, 1.13 ms, 875 TFLOP/s
-// (a large library product: 1140).  One token against a long cache by HBM: sixteen of
-// 6k to 16k keys, 775 MB in 163 us, 4.8 TB/s.
+// Long sequences are bound by the matrix pipe beside the exponentials: 15.5k tokens in
+// two causal documents, bf16, 32 heads of 128 over 8 key heads, 1.11 to 1.18 ms from card
+// to card, 840 to 890 TFLOP/s (a large library product: 1140 to 1160).  With a cap, four
+// such documents of 14.7k tokens and 16 heads run at 630 to 660: the cap's vector work is not
+// hidden behind the products.  At width 128 the 128-row forms spill 2 to 27 registers (4
+// in the plain and the capped one with aligned rows).  One token against a long cache is bound
+// by HBM: sixteen of 6k to 16k keys, 775 MB in 163 us, 4.8 TB/s.
 template <class T, int DP, int WQ, bool CAP, bool EXTRA, bool VEC>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 && DP > 32 ? 1 : 2)
 attn_fwd_kernel(AttnArgs x, FwdShape f) {

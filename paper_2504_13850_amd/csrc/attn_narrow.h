@@ -5,8 +5,11 @@
 // no barrier, and the four waves of a workgroup have different heads or rows.
 //
 // Bound by the vector unit: about 30 instructions a pair forward, most of them
-// the cap's and the softmax's exponentials.  16 sequences of 16 to 256 tokens, fp32,
-// 50 heads of width 2, capped: 28 us forward, 33 and 37 us for the two gradient kernels.
+// the cap's and the softmax's exponentials; the two gradient kernels compute score, cap
+// and exponential again, each.  16 sequences of 16 to 256 tokens, fp32, 50 heads of width
+// 2, capped at 30: 28 us forward, 34 and 37 us for the gradient kernels, 92 us in all
+// where the scores stay below a third of the cap (cap_scores), 123 where they are as
+// large as it, 66 without a cap.
 #pragma once
 
 #include "attn_bwd.h"

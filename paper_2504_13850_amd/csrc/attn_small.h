@@ -7,9 +7,11 @@
 // (P, dP), then dS and dq.  Key phase: P and dS go to LDS where K and V were, and a
 // wave sums them over the queries for 32 keys.
 //
-// Bound by latency (the chain of loads, five products and five barriers).  The
-// BERT-shaped block, 32 x 12 heads, bias and dropout: 25 us; the query and the key
-// kernel took 15 and 22, and a launch more.
+// The BERT-shaped block, 32 x 12 heads, bias and dropout: 25 us for one round of
+// workgroups; the query and the key kernel took 15 and 22, and a launch more.  A wave's
+// 80 matrix instructions are about 2 us of that; the rest (loads, the bias' two dependent
+// loads, generator, diagonal sums, two passes through LDS, five barriers) has not been
+// timed apart.
 #pragma once
 
 #include "attn_bwd.h"

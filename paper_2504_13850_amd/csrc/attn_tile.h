@@ -54,7 +54,10 @@ __device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b
     return c;
 }
 
-// Eight accumulator values as an operand (one rounding to bf16).
+// Eight accumulator values as an operand: probabilities and score gradients, which
+// bf16 calls round once here so that their products run at the bf16 rate, sixteen
+// times fp32's.  Each rounding is independent and below 2^-9 in the root mean square,
+// as large as that of a result; sums over them stay fp32.
 template <class T>
 __device__ __forceinline__ Frag<T> pack8(const float* x);
 template <>
@@ -257,7 +260,7 @@ __device__ __forceinline__ void store_row(T* row, const f32x16* acc, float s, in
 // ------------------------------------------------------------------ scores, base 2
 // u log2(e) = S mul + add, or with a cap cl tanh(cs S) + add.  tanh(y) = 1 - 2 / (e^2y
 // + 1), off by up to 2^-21 where y is far below zero and the quotient near 2: far below
-// a bf16 probability's rounding.  fp32 takes |y| there, whose quotient is small (2^-23
+// a bf16 probability's rounding.  fp32 takes |y| there, whose quotient is small (2^-22
 // at 0.35, less above), and below 0.35, where this form would lose the leading digits,
 // the series of tanh.
 struct ScoreK {

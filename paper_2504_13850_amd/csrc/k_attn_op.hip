@@ -28,7 +28,8 @@ namespace {
 // The table's gradient from the key kernel's sums by distance: a workgroup per
 // head, 256 distances at a time and four groups of threads on the tiles of all
 // sequences, which meet in order; then 32 threads per bucket.  Latency: 4 us for 12 heads
-// and 32 sequences.
+// and 32 sequences.  It grows with the tiles that max_k allows each sequence, there or
+// not: (2 radius + 1) floats each for a head, read by the head's one workgroup.
 template <class T>
 __global__ void __launch_bounds__(1024) bucket_sums(AttnArgs x, int parts) {
     const fo_attn& a = x.a;

@@ -5,7 +5,9 @@
 // generator call (about 70 instructions, a third of them at quarter rate: the
 // chip draws some 2e12 numbers a second, 13 TB/s of bf16 input, residual and
 // output).  65536 x 768 bf16 with residual, 302 MB: 53 us, 5.7 TB/s; a copy of a
-// GiB runs at 5.1.
+// GiB runs at 5.15.  That is for rows that all start 16-byte aligned; one operand whose
+// rows do not (a dense bf16 width that is no multiple of 8) puts the whole call on
+// element by element loads and stores.
 #include <algorithm>
 
 #include "ops.h"
