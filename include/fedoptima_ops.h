@@ -72,7 +72,9 @@ typedef struct {
      * values are not checked: the kernels clamp them to the rows there are and
      * the lengths to max_q and max_k. */
     const int32_t *q_begin, *q_end, *k_begin, *k_end;
-    /* Element (row r, head h, d) of x is at x[r x_ld + h x_hs + d], strides in elements. */
+    /* Element (row r, head h, d) of x is at x[r x_ld + h x_hs + d], strides in
+     * elements; no two elements share an address (FO_EINVAL).  Results share no
+     * memory with operands or with each other. */
     int64_t q_ld, q_hs, k_ld, k_hs, v_ld, v_hs, out_ld, out_hs;
     float scale;                         /* usually 1 / sqrt(head_dim)                         */
     float cap;                           /* >= 0; 0: scores are not capped.  scale log2(e),
