@@ -1,7 +1,9 @@
 /*
  * fedoptima_ops.h -- transformer operators of libfedoptima for networks beyond
  * the built-in configurations: masked attention with its gradients, a learned
- * bias by distance, and dropout.
+ * bias by distance, dropout, and what stands around them in a language model:
+ * embedding, RMS norm, products of 8-bit rows, log probabilities of tokens with
+ * the cross-entropy, and a preference loss.
  *
  * A server that trains a transformer of its own (another width, longer
  * sequences, causal or prefix language models, grouped key heads, dropout)
@@ -151,6 +153,134 @@ FO_API int64_t fo_dropout_workspace(int64_t rows, int32_t cols);
 FO_API fo_status fo_dropout_bwd(int32_t dtype, int64_t rows, int32_t cols, const void* dy, int64_t dy_ld, float p,
                                 uint64_t seed, uint32_t offset, void* dx, int64_t dx_ld, void* dbias,
                                 void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ embedding
+ * out_r = scale table[tokens[r]] over rows of `cols` elements; a token outside
+ * [0, vocab) (padding) has a row of zeros and takes part in no gradient.  tokens:
+ * device int32[rows].  ld: row strides in elements, >= cols.  The product is
+ * rounded once.  Errors: FO_EINVAL, FO_EHIP. */
+FO_API fo_status fo_embed_fwd(int32_t dtype, int64_t rows, int32_t cols, int32_t vocab, const int32_t* tokens,
+                              const void* table, int64_t table_ld, float scale, void* out, int64_t out_ld,
+                              void* hip_stream);
+
+/* dtable_v = scale * the sum of dout's rows of token v, in the order of the rows;
+ * every row of dtable is written (0 for tokens that do not come).  accumulate !=
+ * 0 adds to what dtable holds instead (a table that is the output's weights too)
+ * and leaves the rows of other tokens as they are.  Sums are fp32 and rounded
+ * once, after that addition.  rows up to 2^28. */
+FO_API int64_t fo_embed_workspace(int64_t rows, int32_t cols, int32_t vocab);
+FO_API fo_status fo_embed_bwd(int32_t dtype, int64_t rows, int32_t cols, int32_t vocab, const int32_t* tokens,
+                              const void* dout, int64_t dout_ld, float scale, int32_t accumulate, void* dtable,
+                              int64_t dtable_ld, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ RMS norm
+ * For each row of [rows][cols]:
+ *
+ *   h = x + residual                       residual may be NULL
+ *   rstd = 1 / sqrt(mean h^2 + eps)
+ *   y = h rstd w                           w [cols], may be NULL: ones
+ *
+ * h (may be NULL) and rstd (fp32 [rows], may be NULL) are what the backward pass
+ * needs; h is x itself without a residual.  y is computed from h before h is
+ * rounded.  y or h may be x or residual, with its row stride; y is not h.
+ * eps >= 0.  A row of zeros has y = 0, with eps = 0 too.
+ * Errors: FO_EINVAL, FO_EHIP. */
+FO_API fo_status fo_rmsnorm_fwd(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld,
+                                const void* residual, int64_t res_ld, const void* w, float eps, void* h, int64_t h_ld,
+                                void* y, int64_t y_ld, float* rstd, void* hip_stream);
+
+/* With g = dy w:  dx = dres + rstd (g - h rstd^2 mean(g h)), the gradient of x
+ * and of residual alike, and dw_c = sum over the rows of dy h rstd.  dres (may be
+ * NULL) is the gradient that reaches h on its other way.  h as stored (x without
+ * a residual).  dx may be dy, dres or h, with its row stride.  dw ([cols], may be
+ * NULL) needs the workspace. */
+FO_API int64_t fo_rmsnorm_workspace(int64_t rows, int32_t cols);
+FO_API fo_status fo_rmsnorm_bwd(int32_t dtype, int64_t rows, int32_t cols, const void* dy, int64_t dy_ld,
+                                const void* h, int64_t h_ld, const void* w, const float* rstd, const void* dres,
+                                int64_t dres_ld, void* dx, int64_t dx_ld, void* dw, void* workspace,
+                                int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ 8-bit rows
+ * A row in 8 bits is e4m3 (4 exponent and 3 mantissa bits, no infinity, largest
+ * 448), one byte an element, with one fp32 scale: element c stands for scale
+ * y8[c].  scale = max |y| / 448, and y8 = y 448 / max |y| rounded to nearest even.
+ * A row of zeros has scale 0.  Rows whose largest element is below 2^-100 are
+ * divided by 2^-100 in its place.  A row that holds NaN or infinities gets a scale
+ * or elements that are NaN; other rows do not notice.
+ *
+ * fo_rmsnorm_f8: the forward norm above with y in 8 bits (for the next product, in
+ * passes without a gradient).  fo_quant_f8: the rows of x themselves (weights,
+ * other activations). */
+FO_API fo_status fo_rmsnorm_f8(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld,
+                               const void* residual, int64_t res_ld, const void* w, float eps, void* h, int64_t h_ld,
+                               uint8_t* y8, int64_t y8_ld, float* y_scale, void* hip_stream);
+FO_API fo_status fo_quant_f8(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld, uint8_t* y8,
+                             int64_t y8_ld, float* y_scale, void* hip_stream);
+
+/* c_mn = a_scale[m] b_scale[n] sum_k a_mk b_nk, a [M][K] and b [N][K] in 8 bits,
+ * summed in fp32 and rounded once to dtype.  a_scale [M] and b_scale [N] may be
+ * NULL (ones).  M >= 0; N, K >= 1.  In bf16 calls the products enter those sums by
+ * eights, each cut below 2^-13 of the largest of its eight (the 8-bit matrix
+ * instruction's way: some 1.4e-5 of the result's norm); fp32 calls keep all bits of
+ * the products and take several times as long.  Rows that start 16-byte aligned
+ * with K a multiple of 16 are read faster. */
+FO_API int64_t fo_gemm_f8_workspace(int64_t M, int32_t N, int32_t K);
+FO_API fo_status fo_gemm_f8(int32_t dtype, int64_t M, int32_t N, int32_t K, const uint8_t* a, int64_t lda,
+                            const float* a_scale, const uint8_t* b, int64_t ldb, const float* b_scale, void* c,
+                            int64_t ldc, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ log probabilities
+ * For row r of logits [rows][vocab] with target t = targets[r] (device int32):
+ *
+ *   z = scale logits_r                     scale > 0
+ *   lse[r] = log sum_v exp(z_v)            natural logarithm
+ *   logp[r] = z_t - lse[r]
+ *
+ * A row whose target is outside [0, vocab) is ignored: it is not read, logp = lse =
+ * 0, and its gradient is 0.  Logits of -infinity count as probability 0; a row of
+ * nothing else has logp = lse = -infinity and no gradient.  logp and lse are fp32
+ * (lse may be NULL in the forward call).  The terms other than the target's are
+ * summed apart, so that logp near 0 and its gradient keep their leading bits.
+ * Errors: FO_EINVAL, FO_EHIP. */
+FO_API int64_t fo_logp_workspace(int64_t rows, int32_t vocab);
+FO_API fo_status fo_logp_fwd(int32_t dtype, int64_t rows, int32_t vocab, const void* logits, int64_t ld,
+                             const int32_t* targets, float scale, float* logp, float* lse, void* workspace,
+                             int64_t workspace_bytes, void* hip_stream);
+
+/* dlogits_v = scale dlogp[r] (1{v = t} - exp(z_v - lse)), logp and lse as the
+ * forward call left them.  Every row is written (zeros where it is ignored; its
+ * dlogp is not read).  dlogits may be logits, with its row stride. */
+FO_API fo_status fo_logp_bwd(int32_t dtype, int64_t rows, int32_t vocab, const void* logits, int64_t ld,
+                             const int32_t* targets, float scale, const float* logp, const float* lse,
+                             const float* dlogp, void* dlogits, int64_t dlogits_ld, void* hip_stream);
+
+/* Cross-entropy with its gradient, in one pass over the logits where a row fits
+ * the registers: loss[r] = -logp[r], and dlogits the gradient of sum_r weight[r]
+ * loss[r] (weight: device fp32[rows], not read for ignored rows).  dlogits may be
+ * logits, with its row stride. */
+FO_API fo_status fo_xent(int32_t dtype, int64_t rows, int32_t vocab, const void* logits, int64_t ld,
+                         const int32_t* targets, float scale, const float* weight, float* loss, void* dlogits,
+                         int64_t dlogits_ld, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ preference loss
+ * Pairs of answers whose tokens' log probabilities lie in rows: answer 2 i, the
+ * chosen one of pair i, rows [begin[2 i], end[2 i]); answer 2 i + 1 the rejected
+ * one.
+ *
+ *   reward_q = beta sum over its rows of (logp - ref)      (mean != 0: beta mean)
+ *   d = reward_{2i} - reward_{2i+1}
+ *   loss_i = (1 - smooth) log(1 + exp(-d)) + smooth log(1 + exp(d))
+ *   dlogp = the gradient of dloss sum_i loss_i
+ *
+ * ref (the frozen model's log probabilities) may be NULL: zeros.  An answer without
+ * rows has reward 0.  logp, ref, dlogp: device fp32[rows]; begin, end: device
+ * int32[2 pairs], clamped to the rows; loss fp32[pairs], reward fp32[2 pairs].  No
+ * two answers share rows.  Rows of no answer are neither read nor written.  dlogp
+ * (may be NULL) may be logp.  Sums are fp64.  beta finite, smooth in [0, 1].
+ * Errors: FO_EINVAL, FO_EHIP. */
+FO_API fo_status fo_pref_loss(int32_t pairs, int64_t rows, const int32_t* begin, const int32_t* end, const float* logp,
+                              const float* ref, float beta, float smooth, int32_t mean, float dloss, float* loss,
+                              float* reward, float* dlogp, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,9 @@ EXPORTS = [
     "fo_queues_sender_status", "fo_queues_log_enable", "fo_queues_log_read", "fo_pipeline_run",
     "fo_net_units", "fo_select_split", "fo_aux_network", "fo_attn_workspace", "fo_attn_fwd", "fo_attn_bwd",
     "fo_relpos_buckets", "fo_dropout_fwd", "fo_dropout_workspace", "fo_dropout_bwd",
+    "fo_embed_fwd", "fo_embed_workspace", "fo_embed_bwd", "fo_rmsnorm_fwd", "fo_rmsnorm_workspace", "fo_rmsnorm_bwd",
+    "fo_rmsnorm_f8", "fo_quant_f8", "fo_gemm_f8_workspace", "fo_gemm_f8", "fo_logp_workspace", "fo_logp_fwd",
+    "fo_logp_bwd", "fo_xent", "fo_pref_loss",
 ]
 FO_NET_VGG5, FO_NET_MOBILENETV3_LARGE, FO_NET_TRANSFORMER6, FO_NET_TRANSFORMER12, FO_NET_VGG16 = range(1, 6)
 FO_SCHED_COUNTER, FO_SCHED_FIFO = 0, 1
@@ -178,6 +181,21 @@ def lib():
             "fo_dropout_workspace": (i64, [i64, i32]),
             "fo_dropout_bwd": (C.c_int, [i32, i64, i32, vp, i64, f32, C.c_uint64, C.c_uint32, vp, i64, vp, vp, i64,
                                          vp]),
+            "fo_embed_fwd": (C.c_int, [i32, i64, i32, i32, vp, vp, i64, f32, vp, i64, vp]),
+            "fo_embed_workspace": (i64, [i64, i32, i32]),
+            "fo_embed_bwd": (C.c_int, [i32, i64, i32, i32, vp, vp, i64, f32, i32, vp, i64, vp, i64, vp]),
+            "fo_rmsnorm_fwd": (C.c_int, [i32, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp]),
+            "fo_rmsnorm_workspace": (i64, [i64, i32]),
+            "fo_rmsnorm_bwd": (C.c_int, [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp]),
+            "fo_rmsnorm_f8": (C.c_int, [i32, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, i64, vp, vp]),
+            "fo_quant_f8": (C.c_int, [i32, i64, i32, vp, i64, vp, i64, vp, vp]),
+            "fo_gemm_f8_workspace": (i64, [i64, i32, i32]),
+            "fo_gemm_f8": (C.c_int, [i32, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp]),
+            "fo_logp_workspace": (i64, [i64, i32]),
+            "fo_logp_fwd": (C.c_int, [i32, i64, i32, vp, i64, vp, f32, vp, vp, vp, i64, vp]),
+            "fo_logp_bwd": (C.c_int, [i32, i64, i32, vp, i64, vp, f32, vp, vp, vp, vp, i64, vp]),
+            "fo_xent": (C.c_int, [i32, i64, i32, vp, i64, vp, f32, vp, vp, vp, i64, vp, i64, vp]),
+            "fo_pref_loss": (C.c_int, [i32, i64, vp, vp, vp, vp, f32, f32, i32, f32, vp, vp, vp, vp]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -720,3 +738,191 @@ def fo_dropout_bwd(dy, dx, p: float, seed: int, offset: int, dbias=None, workspa
     _on_gpu("fo_dropout_bwd", dy.get_device(), stream, workspace)
     _check(lib().fo_dropout_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), p, seed, offset, dx.data_ptr(),
                                 _ld(dx), _dptr(dbias), _dptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+# ------------------------------------------------------------------ a language model's step around its attention
+def _row_list(what, n, dt, dev, *tensors):
+    """The given tensors (None apart) are contiguous lists of n numbers of type dt on device dev."""
+    for t in tensors:
+        if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous() or t.get_device() != dev):
+            raise FoError(FO_EINVAL, f"{what}: contiguous {dt} tensors of {n} numbers on the operands' device")
+
+
+def _matrices(what, shape, *tensors):
+    """The given tensors (None apart) are matrices of one shape, with distinct rows."""
+    for t in tensors:
+        if t is not None and (t.dim() != 2 or t.shape != shape):
+            raise FoError(FO_EINVAL, f"{what}: matrices of shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _lds(t) -> int:
+    return 0 if t is None else _ld(t)
+
+
+def _eight_bits(what, dev, *tensors):
+    """The given tensors are e4m3 matrices (or their bytes) on device dev with a contiguous last dimension."""
+    import torch
+    for t in tensors:
+        if (t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.dim() != 2 or t.get_device() != dev
+                or (t.stride(-1) != 1 and t.shape[-1] > 1)):
+            raise FoError(FO_EINVAL, f"{what}: 8-bit rows are float8_e4m3fn or uint8 matrices with a contiguous last dimension")
+
+
+def _workspace(n) -> int:
+    if n < 0:
+        raise FoError(FO_EINVAL, last_error())
+    return n
+
+
+def fo_embed_fwd(tokens, table, out, scale: float = 1.0, stream=None):
+    """out[r] = scale table[tokens[r]], zeros where the token (int32) is outside the table."""
+    _same("fo_embed_fwd", table, table, out)
+    dev, rows = table.get_device(), tokens.numel()
+    _row_list("fo_embed_fwd", rows, _torch_types()[1], dev, tokens)
+    _matrices("fo_embed_fwd", (table.shape[0], table.shape[-1]), table)
+    _matrices("fo_embed_fwd", (rows, table.shape[1]), out)
+    _on_gpu("fo_embed_fwd", dev, stream)
+    _check(lib().fo_embed_fwd(_dtype(table), rows, table.shape[1], table.shape[0], tokens.data_ptr(), table.data_ptr(),
+                              _ld(table), scale, out.data_ptr(), _ld(out), _stream(stream)))
+
+
+def fo_embed_workspace(rows: int, cols: int, vocab: int) -> int:
+    return _workspace(lib().fo_embed_workspace(rows, cols, vocab))
+
+
+def fo_embed_bwd(tokens, dout, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
+    """dtable[v] = scale times the sum of dout's rows of token v (added to what it holds if accumulate)."""
+    _same("fo_embed_bwd", dtable, dtable, dout)
+    dev, rows = dtable.get_device(), tokens.numel()
+    _row_list("fo_embed_bwd", rows, _torch_types()[1], dev, tokens)
+    _matrices("fo_embed_bwd", (dtable.shape[0], dtable.shape[-1]), dtable)
+    _matrices("fo_embed_bwd", (rows, dtable.shape[1]), dout)
+    _on_gpu("fo_embed_bwd", dev, stream, workspace)
+    _check(lib().fo_embed_bwd(_dtype(dtable), rows, dtable.shape[1], dtable.shape[0], tokens.data_ptr(),
+                              dout.data_ptr(), _ld(dout), scale, 1 if accumulate else 0, dtable.data_ptr(),
+                              _ld(dtable), _dptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_rmsnorm_fwd(x, w, y, rstd, eps: float, residual=None, h=None, stream=None):
+    """h = x + residual, rstd = 1 / sqrt(mean h^2 + eps), y = h rstd w; residual, h, w and rstd may be None."""
+    _same("fo_rmsnorm_fwd", x, x, y, residual, h, w)
+    _matrices("fo_rmsnorm_fwd", x.shape, x, y, residual, h)
+    (rows, cols), dev = x.shape, x.get_device()
+    _row_list("fo_rmsnorm_fwd", cols, x.dtype, dev, w)
+    _row_list("fo_rmsnorm_fwd", rows, _torch_types()[2], dev, rstd)
+    _on_gpu("fo_rmsnorm_fwd", dev, stream)
+    _check(lib().fo_rmsnorm_fwd(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _addr(residual), _lds(residual), _addr(w),
+                                eps, _addr(h), _lds(h), y.data_ptr(), _ld(y), _addr(rstd), _stream(stream)))
+
+
+def fo_rmsnorm_workspace(rows: int, cols: int) -> int:
+    return _workspace(lib().fo_rmsnorm_workspace(rows, cols))
+
+
+def fo_rmsnorm_bwd(dy, h, w, rstd, dx, dw=None, dres=None, workspace=None, stream=None):
+    """The gradients of x (and residual) and of w; h and rstd as the forward call left them (h = x without a residual)."""
+    _same("fo_rmsnorm_bwd", dy, dy, h, w, dx, dw, dres)
+    _matrices("fo_rmsnorm_bwd", dy.shape, dy, h, dx, dres)
+    (rows, cols), dev = dy.shape, dy.get_device()
+    _row_list("fo_rmsnorm_bwd", cols, dy.dtype, dev, w, dw)
+    _row_list("fo_rmsnorm_bwd", rows, _torch_types()[2], dev, rstd)
+    _on_gpu("fo_rmsnorm_bwd", dev, stream, workspace)
+    _check(lib().fo_rmsnorm_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h), _addr(w),
+                                rstd.data_ptr(), _addr(dres), _lds(dres), dx.data_ptr(), _ld(dx), _addr(dw),
+                                _addr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_rmsnorm_f8(x, w, y8, y_scale, eps: float, residual=None, h=None, stream=None):
+    """fo_rmsnorm_fwd with y as e4m3 rows and an fp32 scale for each."""
+    _same("fo_rmsnorm_f8", x, x, residual, h, w)
+    _matrices("fo_rmsnorm_f8", x.shape, x, y8, residual, h)
+    (rows, cols), dev = x.shape, x.get_device()
+    _eight_bits("fo_rmsnorm_f8", dev, y8)
+    _row_list("fo_rmsnorm_f8", cols, x.dtype, dev, w)
+    _row_list("fo_rmsnorm_f8", rows, _torch_types()[2], dev, y_scale)
+    _on_gpu("fo_rmsnorm_f8", dev, stream)
+    _check(lib().fo_rmsnorm_f8(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _addr(residual), _lds(residual), _addr(w),
+                               eps, _addr(h), _lds(h), y8.data_ptr(), _ld(y8), y_scale.data_ptr(), _stream(stream)))
+
+
+def fo_quant_f8(x, y8, y_scale, stream=None):
+    """The rows of x as e4m3 with an fp32 scale for each."""
+    _same("fo_quant_f8", x, x)
+    _matrices("fo_quant_f8", x.shape, x, y8)
+    dev = x.get_device()
+    _eight_bits("fo_quant_f8", dev, y8)
+    _row_list("fo_quant_f8", x.shape[0], _torch_types()[2], dev, y_scale)
+    _on_gpu("fo_quant_f8", dev, stream)
+    _check(lib().fo_quant_f8(_dtype(x), x.shape[0], x.shape[1], x.data_ptr(), _ld(x), y8.data_ptr(), _ld(y8),
+                             y_scale.data_ptr(), _stream(stream)))
+
+
+def fo_gemm_f8_workspace(M: int, N: int, K: int) -> int:
+    return _workspace(lib().fo_gemm_f8_workspace(M, N, K))
+
+
+def fo_gemm_f8(a, a_scale, b, b_scale, c, workspace=None, stream=None):
+    """c [M, N] = a [M, K] b [N, K]^T of 8-bit rows times their scales (None: ones)."""
+    _same("fo_gemm_f8", c, c)
+    dev = c.get_device()
+    _eight_bits("fo_gemm_f8", dev, a, b)
+    (M, K), N = a.shape, b.shape[0]
+    _matrices("fo_gemm_f8", (N, K), b)
+    _matrices("fo_gemm_f8", (M, N), c)
+    f32 = _torch_types()[2]
+    _row_list("fo_gemm_f8", M, f32, dev, a_scale)
+    _row_list("fo_gemm_f8", N, f32, dev, b_scale)
+    _on_gpu("fo_gemm_f8", dev, stream, workspace)
+    _check(lib().fo_gemm_f8(_dtype(c), M, N, K, a.data_ptr(), _ld(a), _addr(a_scale), b.data_ptr(), _ld(b),
+                            _addr(b_scale), c.data_ptr(), _ld(c), _addr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_logp_workspace(rows: int, vocab: int) -> int:
+    """Bytes of workspace for fo_logp_fwd and fo_xent."""
+    return _workspace(lib().fo_logp_workspace(rows, vocab))
+
+
+def _logits(what, logits, targets, dlogits, stream, workspace, *lists):
+    _same(what, logits, logits, dlogits)
+    _matrices(what, logits.shape, logits, dlogits)
+    rows, dev = logits.shape[0], logits.get_device()
+    _row_list(what, rows, _torch_types()[1], dev, targets)
+    _row_list(what, rows, _torch_types()[2], dev, *lists)
+    _on_gpu(what, dev, stream, workspace)
+    return _dtype(logits), rows, logits.shape[1], logits.data_ptr(), _ld(logits), targets.data_ptr()
+
+
+def fo_logp_fwd(logits, targets, logp, lse=None, scale: float = 1.0, workspace=None, stream=None):
+    """logp[r] = z_t - log sum exp z of z = scale logits[r], t = targets[r] (0 where t is outside the vocabulary)."""
+    head = _logits("fo_logp_fwd", logits, targets, None, stream, workspace, logp, lse)
+    _check(lib().fo_logp_fwd(*head, scale, logp.data_ptr(), _addr(lse), _addr(workspace), _bytes(workspace),
+                             _stream(stream)))
+
+
+def fo_logp_bwd(logits, targets, logp, lse, dlogp, dlogits, scale: float = 1.0, stream=None):
+    """The gradient of the logits from that of logp; logp and lse as the forward call left them."""
+    head = _logits("fo_logp_bwd", logits, targets, dlogits, stream, None, logp, lse, dlogp)
+    _check(lib().fo_logp_bwd(*head, scale, logp.data_ptr(), lse.data_ptr(), dlogp.data_ptr(), dlogits.data_ptr(),
+                             _ld(dlogits), _stream(stream)))
+
+
+def fo_xent(logits, targets, weight, loss, dlogits, scale: float = 1.0, workspace=None, stream=None):
+    """loss[r] = -logp[r], and dlogits the gradient of sum weight[r] loss[r]."""
+    head = _logits("fo_xent", logits, targets, dlogits, stream, workspace, weight, loss)
+    _check(lib().fo_xent(*head, scale, weight.data_ptr(), loss.data_ptr(), dlogits.data_ptr(), _ld(dlogits),
+                         _addr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fo_pref_loss(logp, ref, begin, end, loss, reward, dlogp=None, beta: float = 0.1, smooth: float = 0.0,
+                 mean: bool = False, dloss: float = 1.0, stream=None):
+    """The preference loss of answers in pairs, rows [begin[q], end[q]) of logp and ref: loss[pair], reward[answer],
+    and dlogp, the gradient of dloss sum loss (rows of no answer are left as they are)."""
+    f32, dev, pairs = _torch_types()[2], logp.get_device(), loss.numel()
+    _row_list("fo_pref_loss", logp.numel(), f32, dev, logp, ref, dlogp)
+    _row_list("fo_pref_loss", 2 * pairs, _torch_types()[1], dev, begin, end)
+    _row_list("fo_pref_loss", pairs, f32, dev, loss)
+    _row_list("fo_pref_loss", 2 * pairs, f32, dev, reward)
+    _on_gpu("fo_pref_loss", dev, stream)
+    _check(lib().fo_pref_loss(pairs, logp.numel(), begin.data_ptr(), end.data_ptr(), logp.data_ptr(), _addr(ref), beta,
+                              smooth, 1 if mean else 0, dloss, loss.data_ptr(), reward.data_ptr(), _addr(dlogp),
+                              _stream(stream)))

@@ -10,7 +10,7 @@
 // element by element loads and stores.
 #include <algorithm>
 
-#include "ops.h"
+#include "row8.h"
 
 namespace fo {
 namespace {
@@ -40,54 +40,6 @@ DropShape drop_shape(int64_t rows, int32_t cols, int64_t most) {
 constexpr int64_t kFwdWgs = 8192, kBwdWgs = 2048;
 
 constexpr int FLY = 4;  // rows of a thread in flight
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// Eight values of a row.  NT: past the caches (see run).
-template <class T, bool NT>
-struct Eight {
-    u32x4 u[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p, int n, bool vec) {
-        if (vec) {
-#pragma unroll
-            for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
-                const u32x4* q = reinterpret_cast<const u32x4*>(p) + c;
-                u[c] = NT ? __builtin_nontemporal_load(q) : *q;
-            }
-        } else {
-            T v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : T(0);
-            __builtin_memcpy(u, v, sizeof(u));
-        }
-    }
-    __device__ __forceinline__ float at(int e) const {
-        T v[8];
-        __builtin_memcpy(v, u, sizeof(u));
-        return to_f(v[e]);
-    }
-    __device__ __forceinline__ static void store(T* p, const float* x, int n, bool vec) {
-        u32x4 w[sizeof(T) / 2];
-        if constexpr (sizeof(T) == 2)
-            w[0] = u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])};
-        else
-            __builtin_memcpy(w, x, sizeof(w));
-        if (vec) {
-#pragma unroll
-            for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
-                u32x4* q = reinterpret_cast<u32x4*>(p) + c;
-                if (NT) __builtin_nontemporal_store(w[c], q);
-                else *q = w[c];
-            }
-        } else {
-            T v[8];
-            __builtin_memcpy(v, w, sizeof(w));
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < n) p[e] = v[e];
-        }
-    }
-};
 
 // BWD: x is dy and y is dx; part (may be NULL) receives the workgroup's column sums.
 template <class T, bool BWD, bool NT>
@@ -157,28 +109,6 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropArgs d, DropShape f, b
     }
 }
 
-// 32 columns a workgroup, the parts dealt to 32 rows of threads and joined in order.
-template <class T>
-__global__ void __launch_bounds__(1024) dbias_kernel(const float* __restrict__ part, int parts, int cols,
-                                                    T* __restrict__ out) {
-    __shared__ float sums[32][32];
-    const int t = threadIdx.x & 31, y = threadIdx.x >> 5, c = block_of() * 32 + t;
-    float s = 0.f;
-    if (c < cols) {
-#pragma unroll 8
-        for (int p = y; p < parts; p += 32) s += part[(int64_t)p * cols + c];
-    }
-    sums[y][t] = s;
-    __syncthreads();
-    if (y || c >= cols) return;
-    for (int k = 1; k < 32; ++k) s += sums[k][t];
-    out[c] = from_f<T>(s);
-}
-
-template <class T>
-bool vec_rows(const void* p, int64_t ld) {
-    return ((uintptr_t)p & 15) == 0 && ld * (int64_t)sizeof(T) % 16 == 0;
-}
 template <class T, bool BWD>
 fo_status run(const DropArgs& d, const DropShape& f, float* part, hipStream_t s) {
     const bool vec = vec_rows<T>(d.x, d.x_ld) && vec_rows<T>(d.y, d.y_ld) && (!d.res || vec_rows<T>(d.res, d.res_ld));
@@ -198,8 +128,7 @@ fo_status bwd(const DropArgs& d, void* dbias, float* ws, hipStream_t s) {
         if (st != FO_OK) return st;
     }
     if (dbias) {
-        dbias_kernel<T><<<grid_of(cdiv(d.cols, 32)), 1024, 0, s>>>(ws, f.parts, d.cols, (T*)dbias);
-        FO_LAUNCHED();
+        return column_sums<T>(ws, f.parts, d.cols, (T*)dbias, s);
     }
     return FO_OK;
 }

@@ -1,0 +1,470 @@
+"""GPU tests of a language model's operators around its attention against their plain 64-bit statements
+(tests/lm_ref.py), on the kernels' own (rounded) inputs, element by element.
+
+Error bounds.  HALF: a result is rounded once to its type, by at most half a step: 2^-8 of its value in bf16, 2^-24 in
+fp32, 2^-4 in e4m3 (or half of its smallest step, 2^-10).  F = 2^-24 bounds each fp32 operation before that.  A sum of n
+terms is off by at most n F times the sum of their sizes, whatever its order; where a sum's terms are dealt to threads
+and joined in a tree, `steps` counts the longest chain of additions.  The hardware's exponential, logarithm and
+reciprocal are within a few steps: 4 F.
+"""
+import numpy as np
+import pytest
+
+from tests import lm_ref as R
+from tests.gpu_util import announce, torch_cuda
+
+pytestmark = pytest.mark.gpu
+A = pytest.importorskip("paper_2504_13850_amd.api")
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+F = 2.0 ** -24
+NAN = float("nan")
+
+
+def _dt(name):
+    torch = torch_cuda()
+    return {"bf16": torch.bfloat16, "f32": torch.float32, "f8": torch.float8_e4m3fn}[name]
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Mat:
+    """A [rows][cols] matrix in memory of its own: `pad` elements between rows, `shift` before the first, all of them
+    NaN (bytes 0x7F in 8 bits), which no call may write."""
+
+    def __init__(self, rows, cols, dtype, pad=0, shift=0, values=None):
+        torch = torch_cuda()
+        self.raw = torch.empty(shift + rows * (cols + pad) + 16, dtype=_dt(dtype) if dtype != "f8" else torch.uint8,
+                               device="cuda")
+        self.raw.fill_(NAN if dtype != "f8" else 0x7F)
+        self.t = self.raw[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        self.inside = torch.zeros(len(self.raw), dtype=torch.bool, device="cuda")
+        self.inside[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols] = True
+        self.f8 = dtype == "f8"
+        if values is not None:
+            self.t.copy_(values)
+
+    def untouched(self):
+        out = self.raw[~self.inside]
+        return bool((out == 0x7F).all() if self.f8 else out.isnan().all())
+
+
+def _normal(seed, *shape, scale=1.0):
+    torch = torch_cuda()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda") * scale
+
+
+def _near(name, got, want, bound):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    bound = np.broadcast_to(np.asarray(bound, np.float64), want.shape)
+    assert got.shape == want.shape
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    with np.errstate(invalid="ignore"):
+        off = ~same & ~(abs(got - want) <= bound + 1e-37)
+    assert not off.any(), (f"{name}: {off.sum()} of {off.size} values off; first at {np.argwhere(off)[0]}: "
+                           f"{got[off][0]!r} for {want[off][0]!r}, bound {bound[off][0]:.3g}")
+
+
+def _ws(n):
+    torch = torch_cuda()
+    return torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") if n else None  # NaN in every float
+
+
+# pad, shift: aligned rows; unaligned ones
+LAYOUTS = [(0, 0), (3, 1)]
+
+
+# ------------------------------------------------------------------ embedding
+EMBED = [(1, 1, 1), (1, 7, 3), (5, 8, 2), (33, 130, 32), (1203, 128, 32), (300, 77, 5000), (4096, 64, 1), (4097, 20, 600),
+         (9000, 24, 40000), (20000, 40, 70), (70000, 8, 1200), (17000, 9, 2200000)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,vocab", EMBED)
+def test_embed(dtype, rows, cols, vocab):
+    torch = torch_cuda()
+    for pad, shift in LAYOUTS if rows * cols < 1 << 17 and vocab < 10000 else LAYOUTS[:1]:
+        announce(f"embed {dtype} {rows} rows of {cols}, vocab {vocab}, pad {pad}")
+        rng = np.random.default_rng(rows + cols)
+        # a few tokens many times, many tokens rarely, some outside the table
+        tok = np.where(rng.random(rows) < 0.3, rng.integers(0, min(vocab, 3), rows), rng.integers(0, vocab, rows))
+        tok = np.where(rng.random(rows) < 0.1, rng.choice([-1, vocab, 2 ** 31 - 1, -2 ** 31], rows), tok).astype(np.int32)
+        tokens = torch.from_numpy(tok).cuda()
+        table = Mat(vocab, cols, dtype, pad, shift, _normal(1, vocab, cols))
+        dout = Mat(rows, cols, dtype, pad, shift, _normal(2, rows, cols))
+        out = Mat(rows, cols, dtype, pad, shift)
+        A.fo_embed_fwd(tokens, table.t, out.t, scale=1.7)
+        want = R.embed(tok, _np(table.t), np.float32(1.7))
+        _near("out", _np(out.t), want, HALF[dtype] * abs(want) * (1 + 2 ** -8))
+        for accumulate in (False, True):
+            dtable = Mat(vocab, cols, dtype, pad, shift, _normal(3, vocab, cols) if accumulate else None)
+            old = _np(dtable.t) if accumulate else None
+            before = dtable.t.clone()
+            A.fo_embed_bwd(tokens, dout.t, dtable.t, scale=1.7, accumulate=accumulate,
+                           workspace=_ws(A.fo_embed_workspace(rows, cols, vocab)))
+            want, size, count = R.embed_grad(tok, _np(dout.t), float(np.float32(1.7)), vocab, old)
+            _near("dtable", _np(dtable.t), want, HALF[dtype] * abs(want) * (1 + 2 ** -8) + (count + 2) * F * size)
+            if accumulate:  # rows of tokens that do not come keep their bits
+                still = np.setdiff1d(np.arange(vocab), tok)
+                assert torch.equal(dtable.t[still].view(torch.uint8), before[still].view(torch.uint8))
+            assert dtable.untouched()
+        assert out.untouched()
+
+
+def test_embed_without_rows():
+    torch = torch_cuda()
+    announce("embed, no rows")
+    tokens, none = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty((0, 8), device="cuda")
+    dtable = torch.ones((5, 8), device="cuda")
+    A.fo_embed_fwd(tokens, dtable, none)
+    A.fo_embed_bwd(tokens, none, dtable, accumulate=True, workspace=_ws(A.fo_embed_workspace(0, 8, 5)))
+    assert (dtable == 1).all()
+    A.fo_embed_bwd(tokens, none, dtable, workspace=_ws(A.fo_embed_workspace(0, 8, 5)))
+    assert (dtable == 0).all()
+
+
+# ------------------------------------------------------------------ RMS norm
+NORM = [(1, 1), (3, 5), (1, 8), (17, 100), (70, 128), (5, 129), (9, 768), (300, 513), (4, 1025), (3, 2050), (6, 4096),
+        (2, 4099), (3, 8200), (2, 16385), (2, 32771), (2100, 64), (1500, 1000)]
+
+
+def _norm_slack(cols):
+    """F times the additions on the longest chain of a row's sum, and a few operations beside it."""
+    return (64 + cols / 1024 + 24) * F
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", NORM)
+def test_norm(dtype, rows, cols):
+    for i, (pad, shift) in enumerate(LAYOUTS):
+        res, weight = (i == 0), (cols != 100)
+        announce(f"norm {dtype} {rows} x {cols}, pad {pad}, residual {res}")
+        mat = lambda seed, scale=1.0: Mat(rows, cols, dtype, pad, shift, _normal(seed, rows, cols, scale=scale))  # noqa: E731
+        x, r = mat(1), mat(2, 3.0) if res else None
+        w = (1 + 0.3 * _normal(3, cols)).to(_dt(dtype)) if weight else None
+        h, y, rstd = Mat(rows, cols, dtype, pad, shift) if res else None, Mat(rows, cols, dtype, pad, shift), _normal(9, rows)
+        A.fo_rmsnorm_fwd(x.t, w, y.t, rstd, 1e-5, residual=r.t if res else None, h=h.t if res else None)
+        wn = None if w is None else _np(w)
+        hh, rr, yy = R.rmsnorm(_np(x.t), _np(r.t) if res else None, wn, float(np.float32(1e-5)))
+        slack = _norm_slack(cols)
+        _near("rstd", _np(rstd), rr, slack * rr)
+        _near("y", _np(y.t), yy, (HALF[dtype] * (1 + 2 ** -8) + slack) * abs(yy))
+        assert y.untouched()
+        if res:
+            _near("h", _np(h.t), hh, HALF[dtype] * abs(hh) * (1 + 2 ** -8) + F * abs(hh))
+            assert h.untouched()
+        # backward, on the stored h
+        hs = h if res else x
+        dy, dres = mat(4), mat(5) if res else None
+        dx, dw = Mat(rows, cols, dtype, pad, shift), _normal(8, cols).to(_dt(dtype))
+        A.fo_rmsnorm_bwd(dy.t, hs.t, w, rstd, dx.t, dw=dw, dres=dres.t if res else None,
+                         workspace=_ws(A.fo_rmsnorm_workspace(rows, cols)))
+        want, wantw, size, sizew = R.rmsnorm_grad(_np(dy.t), _np(hs.t), wn, _np(rstd), _np(dres.t) if res else None)
+        _near("dx", _np(dx.t), want, HALF[dtype] * abs(want) * (1 + 2 ** -8) + slack * size)
+        _near("dw", _np(dw), wantw, HALF[dtype] * abs(wantw) * (1 + 2 ** -8) + (rows + 4) * F * sizew)
+        assert dx.untouched()
+        # without the weight's gradient the same dx
+        again = Mat(rows, cols, dtype, pad, shift)
+        A.fo_rmsnorm_bwd(dy.t, hs.t, w, rstd, again.t, dres=dres.t if res else None)
+        assert (_np(again.t) == _np(dx.t)).all()
+
+
+@pytest.mark.parametrize("cols", [96, 3000, 40000])
+def test_norm_in_place(cols):
+    torch = torch_cuda()
+    announce(f"norm in place, {cols} columns")
+    x, r, w = (_normal(s, 5, cols) for s in (1, 2, 3))
+    w = w[0].contiguous()
+    y, h, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(5, device="cuda")
+    A.fo_rmsnorm_fwd(x, w, y, rstd, 1e-6, residual=r, h=h)
+    x2, r2 = x.clone(), r.clone()
+    A.fo_rmsnorm_fwd(x2, w, x2, None, 1e-6, residual=r2, h=r2)
+    assert torch.equal(x2, y) and torch.equal(r2, h)
+    x2, r2 = x.clone(), r.clone()
+    A.fo_rmsnorm_fwd(x2, w, r2, None, 1e-6, residual=r2, h=x2)
+    assert torch.equal(r2, y) and torch.equal(x2, h)
+    dy, dres, dx, dw = _normal(4, 5, cols), _normal(5, 5, cols), torch.empty_like(x), torch.empty_like(w)
+    ws = _ws(A.fo_rmsnorm_workspace(5, cols))
+    A.fo_rmsnorm_bwd(dy, h, w, rstd, dx, dw=dw, dres=dres, workspace=ws)
+    for over in range(3):
+        v, dw2 = [dy.clone(), dres.clone(), h.clone()], torch.empty_like(w)
+        A.fo_rmsnorm_bwd(v[0], v[2], w, rstd, v[over], dw=dw2, dres=v[1], workspace=ws)
+        assert torch.equal(v[over], dx) and torch.equal(dw2, dw)
+
+
+def test_norm_edges():
+    """Rows of zeros with eps = 0, rows with NaN or infinity beside others, no rows."""
+    torch = torch_cuda()
+    announce("norm, edges")
+    x = _normal(1, 6, 200)
+    x[1], x[2, 7], x[4, 199] = 0, NAN, float("inf")
+    y, rstd, q, s = torch.empty_like(x), torch.empty(6, device="cuda"), torch.empty((6, 200), dtype=torch.uint8, device="cuda"), torch.empty(6, device="cuda")
+    A.fo_rmsnorm_fwd(x, None, y, rstd, 0.0)
+    A.fo_rmsnorm_f8(x, None, q, s, 0.0)
+    assert (y[1] == 0).all() and rstd[1] == 0 and s[1] == 0 and (q[1] == 0).all()
+    assert y[2].isnan().all() and y[4, 199].isnan()
+    good = [0, 3, 5]
+    _near("y", _np(y[good]), R.rmsnorm(_np(x[good]), None, None, 0.0)[2], 1e-5)
+    _near("scale", _np(s[good]), R.f8_scale(R.rmsnorm(_np(x[good]), None, None, 0.0)[2]), 1e-7)
+    dx, dw = torch.empty_like(x[:1]), torch.empty(200, device="cuda")
+    A.fo_rmsnorm_bwd(_normal(2, 1, 200), x[1:2], None, rstd[1:2], dx, dw=dw, workspace=_ws(A.fo_rmsnorm_workspace(1, 200)))
+    assert (dx == 0).all() and (dw == 0).all()
+    none = torch.empty((0, 200), device="cuda")
+    A.fo_rmsnorm_fwd(none, None, none.clone(), rstd[:0], 0.0)
+    dw.fill_(1)
+    A.fo_rmsnorm_bwd(none, none, None, rstd[:0], none.clone(), dw=dw, workspace=_ws(A.fo_rmsnorm_workspace(0, 200)))
+    assert (dw == 0).all()
+
+
+# ------------------------------------------------------------------ 8-bit rows
+def _check_f8(y, q, s, slack):
+    """Bytes q and scales s against the 64-bit rows y: half a step of e4m3 each, and what fp32 adds."""
+    scale = R.f8_scale(y)
+    _near("scale", s, scale, (slack + 2 * F) * scale)
+    v = R.f8_values()[q]
+    assert not np.isnan(v).any()
+    unit = y / np.where(scale > 0, scale, 1)[:, None]
+    _near("q", v, unit, 2.0 ** -4 * abs(unit) * (1 + 2 ** -8) + 2.0 ** -10 + 2 * slack * abs(unit))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", NORM)
+def test_f8(dtype, rows, cols):
+    torch = torch_cuda()
+    for pad, shift in LAYOUTS:
+        announce(f"8-bit rows {dtype} {rows} x {cols}, pad {pad}")
+        x = Mat(rows, cols, dtype, pad, shift, _normal(1, rows, cols) * _normal(6, rows, 1).exp())
+        x.t[0] = 0 if rows > 2 else x.t[0]
+        r = Mat(rows, cols, dtype, pad, shift, _normal(2, rows, cols))
+        w = (1 + 0.3 * _normal(3, cols)).to(_dt(dtype))
+        q, s = Mat(rows, cols, "f8", pad, shift), _normal(7, rows)
+        A.fo_quant_f8(x.t, q.t, s)
+        _check_f8(_np(x.t), q.t.cpu().numpy(), _np(s), 4 * F)
+        assert q.untouched()
+        q, h = Mat(rows, cols, "f8", pad, shift), Mat(rows, cols, dtype, pad, shift)
+        A.fo_rmsnorm_f8(x.t, w, q.t, s, 1e-6, residual=r.t, h=h.t)
+        hh, _, yy = R.rmsnorm(_np(x.t), _np(r.t), _np(w), float(np.float32(1e-6)))
+        _check_f8(yy, q.t.cpu().numpy(), _np(s), _norm_slack(cols))
+        _near("h", _np(h.t), hh, (HALF[dtype] * (1 + 2 ** -8) + F) * abs(hh))
+        assert q.untouched() and h.untouched()
+
+
+def test_f8_rounding():
+    """Every e4m3 value comes back as itself, ties go to the even neighbour, and tiny rows keep within their range."""
+    torch = torch_cuda()
+    announce("8-bit rounding")
+    v = R.f8_values()
+    fine = np.sort(np.unique(v[~np.isnan(v)]))
+    mid = (fine[1:] + fine[:-1]) / 2  # exact in fp32
+    rows = np.concatenate([fine, mid, [448.0]])[None].astype(np.float32)
+    x = torch.from_numpy(np.concatenate([rows, rows * 2.0 ** -60])).cuda()
+    q, s = torch.empty(x.shape, dtype=torch.uint8, device="cuda"), torch.empty(2, device="cuda")
+    A.fo_quant_f8(x, q, s)
+    got = R.f8_values()[q.cpu().numpy()]
+    assert s.tolist() == [1.0, 2.0 ** -60]
+    # the neighbour whose last mantissa bit is 0: bytes order the values of a sign
+    byte = {float(b): i for i, b in enumerate(v) if not np.isnan(b)}
+    even = [a if byte[float(abs(a))] % 2 == 0 else b for a, b in zip(fine[:-1], fine[1:])]
+    want = np.concatenate([fine, even, [448.0]])
+    assert (got == want).all()
+    x = torch.full((1, 9), 2.0 ** -120, device="cuda")
+    A.fo_quant_f8(x, q[:1, :9].contiguous(), s[:1])
+    assert s[0] == float(np.float32(2.0 ** -100 / 448))
+
+
+# ------------------------------------------------------------------ 8-bit product
+GEMM = [(1, 1, 1), (1, 5, 16), (3, 64, 128), (7, 100, 77), (16, 16, 4096), (1, 4096, 512), (5, 130, 2064), (33, 257, 384),
+        (64, 512, 1024), (65, 300, 100), (130, 129, 640), (257, 640, 256), (300, 1000, 1500), (520, 513, 2048),
+        (1030, 768, 912), (2, 20, 9001)]
+
+
+def _bytes(seed, rows, cols):
+    """Random bytes, none of them NaN."""
+    b = np.random.default_rng(seed).integers(0, 256, (rows, cols)).astype(np.uint8)
+    return np.where((b & 0x7F) == 0x7F, b ^ 1, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", GEMM)
+def test_gemm_f8(dtype, M, N, K):
+    """In bf16 the matrix instruction adds eight products at a time and cuts each below 2^-13 of the largest of them:
+    seven products lose at most that each, 7 2^-13 < 2^-10 of the terms' sizes.  fp32 calls do not use it."""
+    torch = torch_cuda()
+    v = R.f8_values()
+    cut = 2.0 ** -10 if dtype == "bf16" else 0.0
+    for pad, shift in [(0, 0), (16, 16), (3, 1)]:
+        announce(f"8-bit product {dtype} {M} x {N} x {K}, pad {pad}")
+        a, b = _bytes(M + K, M, K), _bytes(N + 7, N, K)
+        am, bm = (Mat(len(x), K, "f8", pad, shift, torch.from_numpy(x).cuda()) for x in (a, b))
+        sa, sb = (None, None) if pad == 3 else (_normal(1, M).abs() + 0.1, _normal(2, N))
+        c = Mat(M, N, dtype, pad, shift)
+        A.fo_gemm_f8(am.t, sa, bm.t, sb, c.t, workspace=_ws(A.fo_gemm_f8_workspace(M, N, K)))
+        want, size = R.gemm(v[a], None if sa is None else _np(sa), v[b], None if sb is None else _np(sb))
+        _near("c", _np(c.t), want, HALF[dtype] * abs(want) * (1 + 2 ** -8) + ((K + 4) * F + cut) * size)
+        assert c.untouched()
+
+
+def test_gemm_f8_nan_keeps_to_its_row():
+    torch = torch_cuda()
+    announce("8-bit product, NaN")
+    for K in (96, 512):
+        a, b = _bytes(1, 70, K), _bytes(2, 90, K)
+        a[3, 5] = 0x7F
+        b[80, K - 1] = 0xFF
+        c = torch.empty((70, 90), device="cuda")
+        A.fo_gemm_f8(torch.from_numpy(a).cuda(), None, torch.from_numpy(b).cuda(), None, c,
+                     workspace=_ws(A.fo_gemm_f8_workspace(70, 90, K)))
+        bad = np.zeros((70, 90), bool)
+        bad[3], bad[:, 80] = True, True
+        assert (np.isnan(_np(c)) == bad).all()
+
+
+# ------------------------------------------------------------------ log probabilities
+LOGP = [(1, 1), (1, 2), (5, 7), (3, 8), (70, 33), (300, 1000), (9, 1025), (600, 2049), (4, 8192), (520, 8200), (600, 16384),
+        (3, 32000), (530, 32001), (2, 50000), (515, 66001), (1, 128000), (513, 131073), (1, 300001)]
+
+
+def _logits(dtype, rows, vocab, pad, shift, seed=1):
+    """Logits of a spread of 2.5 with targets that some rows are nearly sure of, rows without a target, logits of
+    -infinity, and the target among them once."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(seed + rows + vocab)
+    x = _normal(seed, rows, vocab, scale=2.5)
+    t = rng.integers(0, vocab, rows)
+    sure = torch.from_numpy(rng.random(rows) < 0.4).cuda()
+    x[torch.arange(rows), torch.from_numpy(t)] += torch.where(sure, 22.0, 0.0)
+    if vocab > 4:
+        x[:, rng.integers(0, vocab, 2)] = -float("inf")
+    if rows > 4:
+        t[1], t[2], t[3] = -1, vocab, -2 ** 31
+        x[2] = NAN  # not read
+        x[4] = -float("inf")  # nothing there
+    return Mat(rows, vocab, dtype, pad, shift, x), torch.from_numpy(t.astype(np.int32)).cuda(), t
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", LOGP)
+def test_logp(dtype, rows, vocab):
+    torch = torch_cuda()
+    for pad, shift in LAYOUTS if rows * vocab < 1 << 20 else LAYOUTS[1:]:
+        scale = 0.8 if pad else 1.0
+        announce(f"logp {dtype} {rows} x {vocab}, pad {pad}")
+        x, targets, t = _logits(dtype, rows, vocab, pad, shift)
+        ws = _ws(A.fo_logp_workspace(rows, vocab))
+        logp, lse = torch.full((2, rows), NAN, device="cuda")
+        A.fo_logp_fwd(x.t, targets, logp, lse, scale=scale, workspace=ws)
+        sc, z = float(np.float32(scale)), _np(x.t)
+        z[~((t >= 0) & (t < vocab))] = 0
+        lp, ls, p, miss, there, none = R.logp(z, t, sc)
+        live = there & ~none
+        with np.errstate(invalid="ignore"):
+            spread = np.where(live, sc * (np.where(np.isfinite(z), z, -np.inf).max(1) - np.where(np.isfinite(z), z, np.inf).min(1)), 0)
+            zt = z[np.arange(rows), np.where(there, t, 0)] * sc
+            gap = np.where(live & np.isfinite(zt), sc * np.where(np.isfinite(z), z, -np.inf).max(1) - zt, 0)
+        # the terms' relative error: their arguments' rounding, the exponential, the longest chain of additions
+        c = (64 + vocab / 1024 + 3 * spread) * F
+        away = (gap > 0) * (gap + np.log(vocab) + 1)
+        _near("logp", _np(logp), lp, c * np.where(live, miss, 0) + 4 * F * (np.where(np.isfinite(lp), abs(lp), 0) + away))
+        _near("lse", _np(lse), ls, c + 4 * F * np.where(live, abs(ls) + np.log(vocab), 0))
+        alone = torch.full((rows,), NAN, device="cuda")
+        A.fo_logp_fwd(x.t, targets, alone, scale=scale, workspace=ws)
+        assert torch.equal(alone.view(torch.int32), logp.view(torch.int32))
+        # gradient, by two calls and by one
+        g = _normal(5, rows)
+        if rows > 4:
+            g[1] = NAN  # an ignored row's is not read
+        d = Mat(rows, vocab, dtype, pad, shift)
+        A.fo_logp_bwd(x.t, targets, logp, lse, g, d.t, scale=scale)
+        want = R.logp_grad(z, t, sc, np.where(there, _np(g), 0))
+        big = np.where(live, abs(np.where(np.isfinite(z), z, 0)).max(1) * sc + np.where(live, abs(ls), 0), 0)
+        # the target's factor comes from logp, whose error is above
+        own = np.zeros_like(want)
+        off = c * np.where(live, miss, 0) + 4 * F * (np.where(np.isfinite(lp), np.minimum(abs(lp), 1), 0) + away * (1 - miss))
+        own[np.arange(rows), np.where(there, t, 0)] = np.where(live, abs(sc * np.where(there, _np(g), 0)) * off, 0)
+        _near("dlogits", _np(d.t), want, abs(want) * (HALF[dtype] * (1 + 2 ** -8) + (c + 4 * F * big + 16 * F)[:, None]) + own)
+        assert d.untouched()
+        loss, e = torch.full((rows,), NAN, device="cuda"), Mat(rows, vocab, dtype, pad, shift)
+        A.fo_xent(x.t, targets, -g, loss, e.t, scale=scale, workspace=ws)
+        _near("loss", _np(loss), -lp, c * np.where(live, miss, 0) + 4 * F * (np.where(np.isfinite(lp), abs(lp), 0) + away))
+        _near("dlogits of the loss", _np(e.t), want,
+              abs(want) * (HALF[dtype] * (1 + 2 ** -8) + (c + 4 * F * big + 16 * F)[:, None]) + own)
+        assert e.untouched()
+        # over the logits themselves
+        kept = x.t.clone()
+        A.fo_logp_bwd(x.t, targets, logp, lse, g, x.t, scale=scale)
+        assert torch.equal(x.t, d.t) and x.untouched()
+        x.t.copy_(kept)
+        A.fo_xent(x.t, targets, -g, loss, x.t, scale=scale, workspace=ws)
+        assert torch.equal(x.t, e.t) and x.untouched()
+
+
+def test_logp_nan_keeps_to_its_row():
+    torch = torch_cuda()
+    announce("logp, NaN and infinity")
+    for rows, vocab in ((6, 40), (6, 3000), (6, 20000), (600, 9000)):
+        x = _normal(1, rows, vocab)
+        x[1, vocab - 1], x[3, 0], x[4, 5] = NAN, float("inf"), NAN
+        t = torch.full((rows,), 5, dtype=torch.int32, device="cuda")
+        ws, logp, d = _ws(A.fo_logp_workspace(rows, vocab)), torch.empty(rows, device="cuda"), torch.empty_like(x)
+        A.fo_logp_fwd(x, t, logp, workspace=ws)
+        bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+        bad[[1, 4]] = True
+        assert torch.equal(logp.isnan() | (logp == -float("inf")), bad | (torch.arange(rows, device="cuda") == 3))
+        A.fo_xent(x, t, torch.ones(rows, device="cuda"), logp, d, workspace=ws)
+        assert d[1].isnan().any() and d[4].isnan().any() and not d[[0, 2, 5]].isnan().any()
+
+
+# ------------------------------------------------------------------ preference loss
+@pytest.mark.parametrize("lens,beta,smooth,mean,ref", [
+    ([(1, 1)], 0.1, 0.0, False, True), ([(3, 0), (0, 0), (5, 400)], 0.3, 0.1, False, True),
+    ([(1000, 700), (64, 65), (1, 2)], 0.1, 0.0, True, True), ([(20, 9000)], 0.5, 0.5, False, False),
+    ([(30, 40)] * 300, 2.0, 0.25, False, True), ([(0, 7)], 0.0, 1.0, True, False), ([(4000, 4000)], -3.0, 0.0, False, True)])
+@pytest.mark.parametrize("gap", [0, 2])
+def test_pref(lens, beta, smooth, mean, ref, gap):
+    torch = torch_cuda()
+    announce(f"preference loss of {len(lens)} pairs, gap {gap}")
+    spans, at = [], gap
+    for pair in lens:
+        for n in pair:
+            spans.append((at, at + n))
+            at += n + gap
+    rows = at
+    logp, rf = -_normal(1, rows).abs() * 2, (-_normal(2, rows).abs() * 2 if ref else None)
+    if gap:  # rows of no answer are not read
+        free = np.setdiff1d(np.arange(rows), np.concatenate([np.arange(*s) for s in spans]))
+        logp[free] = NAN
+    on = lambda i: torch.tensor([s[i] for s in spans], dtype=torch.int32, device="cuda")  # noqa: E731
+    loss, reward, d = torch.empty(len(lens), device="cuda"), torch.empty(2 * len(lens), device="cuda"), torch.full((rows,), NAN, device="cuda")
+    kw = dict(beta=beta, smooth=smooth, mean=mean, dloss=0.25)
+    A.fo_pref_loss(logp, rf, on(0), on(1), loss, reward, d, **kw)
+    b, sm = float(np.float32(beta)), float(np.float32(smooth))
+    wl, wr, wd, size, dd = R.pref(_np(logp), None if rf is None else _np(rf), spans, b, sm, mean, 0.25)
+    top = np.abs(dd).max() if len(dd) else 0
+    _near("reward", _np(reward), wr, 2 * F * abs(wr))
+    # d is rounded once, its functions have a few roundings each; d's rounding moves them by that much of themselves
+    _near("loss", _np(loss), wl, (12 + 2 * top) * F * wl)
+    _near("dlogp", _np(d), wd, np.where(np.isnan(size), 0, (12 + 2 * top) * F * size))
+    only = torch.empty_like(loss)
+    A.fo_pref_loss(logp, rf, on(0), on(1), only, reward, None, **kw)
+    assert torch.equal(only, loss)
+    over = logp.clone()
+    A.fo_pref_loss(over, rf, on(0), on(1), only, reward, over, **kw)
+    assert torch.equal(over[~d.isnan()], d[~d.isnan()]) and torch.equal(only, loss)
+
+
+def test_pref_clamps_its_rows():
+    """Bounds outside the rows are cut to them: nothing outside is read or written."""
+    torch = torch_cuda()
+    announce("preference loss, rows outside")
+    raw = torch.full((40,), NAN, device="cuda")
+    logp = raw[8:32]
+    logp.copy_(-_normal(1, 24).abs())
+    d = torch.full((40,), NAN, device="cuda")
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    loss, reward = torch.empty(2, device="cuda"), torch.empty(4, device="cuda")
+    A.fo_pref_loss(logp, None, i32(-5, 10, 20, 2 ** 31 - 1), i32(10, 18, 99, 2 ** 31 - 1), loss, reward, d[8:32])
+    wl, wr, wd, _, _ = R.pref(_np(logp), None, [(0, 10), (10, 18), (20, 24), (24, 24)], float(np.float32(0.1)), 0, False, 1.0)
+    _near("reward", _np(reward), wr, 4 * F * abs(wr))
+    assert (np.isnan(_np(d[8:32])) == np.isnan(wd)).all() and d[:8].isnan().all() and d[32:].isnan().all()

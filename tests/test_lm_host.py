@@ -1,0 +1,259 @@
+"""CPU tests of a language model's operators around its attention: the plain statements' gradients against differences,
+and what the entry points and the binding refuse (before any launch, so no GPU is touched)."""
+import math
+import types
+
+import numpy as np
+import pytest
+import torch
+
+from tests import lm_ref as R
+
+A = pytest.importorskip("paper_2504_13850_amd.api")
+BF16, F32, I32, U8, F8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
+
+
+def _differences(f, x, grad, rng):
+    """Central differences along a random direction: 64 bits, step 1e-5, so their error is about 1e-10 of the curvature;
+    1e-6 is asked."""
+    d = rng.standard_normal(x.shape)
+    want = (f(x + 1e-5 * d) - f(x - 1e-5 * d)) / 2e-5
+    assert abs((grad * d).sum() - want) <= 1e-6 * max(1, abs(want))
+
+
+def test_reference_gradients_against_differences():
+    rng = np.random.default_rng(3)
+    n = rng.standard_normal
+    table, tok, dout = n((6, 4)), np.array([1, 5, -1, 1, 6, 0]), n((6, 4))
+    _differences(lambda t: (R.embed(tok, t, 1.3) * dout).sum(), table, R.embed_grad(tok, dout, 1.3, 6)[0], rng)
+    x, res, w, dy, dres = n((5, 7)), n((5, 7)), n(7), n((5, 7)), n((5, 7))
+
+    def norm(x, w):
+        h, _, y = R.rmsnorm(x, res, w, 0.1)
+        return (y * dy).sum() + (h * dres).sum()
+
+    h, rstd, _ = R.rmsnorm(x, res, w, 0.1)
+    dx, dw, _, _ = R.rmsnorm_grad(dy, h, w, rstd, dres)
+    _differences(lambda v: norm(v, w), x, dx, rng)
+    _differences(lambda v: norm(x, v), w, dw, rng)
+    logits, t, g = 3 * n((6, 9)), np.array([0, 8, -1, 9, 4, 4]), n(6)
+    logits[4, 4] += 9
+    _differences(lambda z: (R.logp(z, t, 0.7)[0] * g).sum(), logits, R.logp_grad(logits, t, 0.7, g), rng)
+    lp, ref, spans = n(12), n(12), [(0, 3), (3, 4), (4, 4), (6, 11)]
+    for mean in (False, True):
+        got = R.pref(lp, ref, spans, 0.6, 0.2, mean, 1.7)[2]
+        _differences(lambda v: 1.7 * R.pref(v, ref, spans, 0.6, 0.2, mean, 1.7)[0].sum(), lp, np.nan_to_num(got), rng)
+
+
+def test_reference_bytes():
+    """The 8-bit values against torch's type, and the softmax's parts against their sum."""
+    v = torch.arange(256, dtype=U8).view(F8).double().numpy()
+    got = R.f8_values()
+    assert (np.isnan(v) == np.isnan(got)).all() and (v == got)[~np.isnan(v)].all()
+    lp, lse, p, miss, _, _ = R.logp(np.array([[0.0, 1.0, -np.inf]]), np.array([1]), 1.0)
+    assert abs(p.sum() - 1) < 1e-15 and abs(miss[0] - p[0, 0]) < 1e-15 and abs(math.exp(lp[0]) - p[0, 1]) < 1e-15
+    assert abs(lse[0] - math.log(1 + math.e)) < 1e-15
+
+
+X = np.zeros(256, np.int64).ctypes.data  # host addresses: never launched
+MANY = (1 << 31) - 1
+CALLS = {  # arguments by name in the call's order
+    "fo_embed_fwd": dict(dt=0, rows=4, cols=8, vocab=5, tokens=X, table=X, table_ld=8, scale=1.0, out=X + 64, out_ld=8, s=None),
+    "fo_embed_bwd": dict(dt=0, rows=4, cols=8, vocab=5, tokens=X, dout=X, dout_ld=8, scale=1.0, accumulate=0, dtable=X + 64,
+                         dtable_ld=8, ws=X, n=1 << 40, s=None),
+    "fo_rmsnorm_fwd": dict(dt=1, rows=4, cols=8, x=X, x_ld=8, res=X + 64, res_ld=8, w=X, eps=0.0, h=X + 128, h_ld=8, y=X + 192,
+                           y_ld=8, rstd=X, s=None),
+    "fo_rmsnorm_bwd": dict(dt=0, rows=4, cols=8, dy=X, dy_ld=8, h=X + 64, h_ld=8, w=X, rstd=X, dres=X + 128, dres_ld=8,
+                           dx=X + 192, dx_ld=8, dw=X, ws=X, n=1 << 40, s=None),
+    "fo_rmsnorm_f8": dict(dt=0, rows=4, cols=8, x=X, x_ld=8, res=None, res_ld=0, w=None, eps=1e-6, h=None, h_ld=0, y=X + 192,
+                          y_ld=8, y_scale=X, s=None),
+    "fo_quant_f8": dict(dt=0, rows=4, cols=8, x=X, x_ld=8, y=X + 192, y_ld=8, y_scale=X, s=None),
+    "fo_gemm_f8": dict(dt=0, rows=4, cols=8, K=16, a=X, lda=16, a_scale=X, b=X + 64, ldb=16, b_scale=X, c=X + 192, ldc=8,
+                       ws=X, n=1 << 40, s=None),
+    "fo_logp_fwd": dict(dt=1, rows=4, cols=8, x=X, x_ld=8, targets=X, scale=1.0, logp=X, lse=X, ws=X, n=1 << 40, s=None),
+    "fo_logp_bwd": dict(dt=1, rows=4, cols=8, x=X, x_ld=8, targets=X, scale=1.0, logp=X, lse=X, dlogp=X, d=X + 64, d_ld=8,
+                        s=None),
+    "fo_xent": dict(dt=1, rows=4, cols=8, x=X, x_ld=8, targets=X, scale=1.0, weight=X, loss=X, d=X + 64, d_ld=8, ws=X,
+                    n=1 << 40, s=None),
+    "fo_pref_loss": dict(pairs=2, rows=4, begin=X, end=X, logp=X, ref=X, beta=0.1, smooth=0.0, mean=0, dloss=1.0, loss=X,
+                         reward=X, dlogp=X, s=None),
+}
+OPTIONAL = {"res", "w", "h", "rstd", "dres", "dw", "a_scale", "b_scale", "lse", "ref", "dlogp", "s", "n"}
+
+
+def _call(name, **kw):
+    args = {**CALLS[name], **kw}
+    assert set(args) == set(CALLS[name])
+    return getattr(A.lib(), name)(*args.values())
+
+
+def _bad(name):
+    """Every argument out of its range, one at a time."""
+    a = CALLS[name]
+    for k, v in a.items():
+        if k in ("s", "accumulate", "mean", "n"):
+            continue
+        if isinstance(v, int) and v >= X:  # an address
+            if k not in OPTIONAL or (name, k) == ("fo_logp_bwd", "lse") or (name, k) == ("fo_logp_bwd", "dlogp"):
+                if k != "ws" or _workspace(name):
+                    yield {k: None}
+            if not (name in ("fo_gemm_f8",) and k in ("a", "b")) and not (name in ("fo_rmsnorm_f8", "fo_quant_f8") and k == "y"):
+                yield {k: v + 1}  # between elements
+        elif k.endswith("ld") or k in ("lda", "ldb", "ldc"):
+            if a.get(k[:-3] if k.endswith("_ld") else k[2:]) is not None:
+                yield {k: v - 1}
+                yield {k: (1 << 31) + 1}
+        elif k == "dt":
+            yield {k: 2}
+            yield {k: -1}
+        elif k in ("rows", "pairs"):
+            yield {k: -1}
+        elif k in ("cols", "vocab", "K"):
+            yield {k: 0}
+        elif isinstance(v, float):
+            yield {k: math.nan}
+            yield {k: math.inf}
+    if "rows" in a and name != "fo_pref_loss":
+        yield {"rows": MANY + 1}
+    for k in ("scale", "eps", "smooth"):
+        if k in a and name not in ("fo_embed_fwd", "fo_embed_bwd"):
+            yield {k: -0.5}
+    if "smooth" in a:
+        yield {"smooth": 1.5}
+
+
+def _workspace(name):
+    """Whether the call's sizes need one."""
+    if name == "fo_embed_bwd":
+        return A.fo_embed_workspace(4, 8, 5)
+    if name == "fo_rmsnorm_bwd":
+        return A.fo_rmsnorm_workspace(4, 8)
+    return A.fo_gemm_f8_workspace(4, 8, 16) if name == "fo_gemm_f8" else A.fo_logp_workspace(4, 8)
+
+
+@pytest.mark.parametrize("name,bad", [(n, b) for n in CALLS for b in _bad(n)], ids=str)
+def test_refuses(name, bad):
+    assert _call(name, **bad) == A.FO_EINVAL and name in A.last_error()
+
+
+@pytest.mark.parametrize("name,bad", [
+    ("fo_rmsnorm_fwd", dict(y=X + 128)), ("fo_rmsnorm_fwd", dict(h=X, h_ld=9)), ("fo_rmsnorm_fwd", dict(y=X + 64, y_ld=9)),
+    ("fo_rmsnorm_f8", dict(y=X)), ("fo_quant_f8", dict(y=X)), ("fo_rmsnorm_bwd", dict(dx=X, dx_ld=9)),
+    ("fo_rmsnorm_bwd", dict(dx=X + 64, dx_ld=9)), ("fo_rmsnorm_bwd", dict(dx=X + 128, dx_ld=9)),
+    ("fo_logp_bwd", dict(d=X, d_ld=9)), ("fo_xent", dict(d=X, d_ld=9)), ("fo_gemm_f8", dict(c=X)),
+    ("fo_gemm_f8", dict(c=X + 64)), ("fo_embed_fwd", dict(out=X)), ("fo_embed_bwd", dict(dtable=X)),
+    ("fo_embed_bwd", dict(rows=(1 << 28) + 1)), ("fo_rmsnorm_bwd", dict(n=8)), ("fo_rmsnorm_bwd", dict(ws=X + 4)),
+    ("fo_rmsnorm_fwd", dict(rows=MANY, x_ld=1 << 31)), ("fo_logp_bwd", dict(rows=MANY, d_ld=1 << 31)),
+    ("fo_xent", dict(rows=4, cols=1 << 20, x_ld=1 << 20, d_ld=1 << 20, n=16))], ids=str)
+def test_refuses_together(name, bad):
+    assert _call(name, **bad) == A.FO_EINVAL and name in A.last_error()
+
+
+def test_accepts_no_rows():
+    none = dict(rows=0)
+    assert _call("fo_embed_fwd", **none, tokens=None, table=None, out=None) == A.FO_OK
+    assert _call("fo_embed_bwd", **none, tokens=None, dout=None, accumulate=1) == A.FO_OK
+    assert _call("fo_rmsnorm_fwd", **none, x=None, res=None, h=None, y=None) == A.FO_OK
+    assert _call("fo_rmsnorm_bwd", **none, dy=None, h=None, rstd=None, dx=None, dw=None, dres=None) == A.FO_OK
+    assert _call("fo_quant_f8", **none, x=None, y=None, y_scale=None) == A.FO_OK
+    assert _call("fo_gemm_f8", **none, a=None, b=None, c=None) == A.FO_OK
+    assert _call("fo_logp_fwd", **none, x=None, targets=None, logp=None) == A.FO_OK
+    assert _call("fo_logp_bwd", **none, x=None, targets=None, logp=None, lse=None, dlogp=None, d=None) == A.FO_OK
+    assert _call("fo_xent", **none, x=None, targets=None, weight=None, loss=None, d=None) == A.FO_OK
+    assert _call("fo_pref_loss", pairs=0, begin=None, end=None, logp=None, ref=None, loss=None, reward=None, dlogp=None) == A.FO_OK
+
+
+@pytest.mark.parametrize("call", [lambda: A.fo_embed_workspace(-1, 8, 8), lambda: A.fo_embed_workspace(1 << 29, 8, 8),
+                                  lambda: A.fo_embed_workspace(4, 0, 8), lambda: A.fo_embed_workspace(4, 8, 0),
+                                  lambda: A.fo_rmsnorm_workspace(-1, 8), lambda: A.fo_rmsnorm_workspace(4, 0),
+                                  lambda: A.fo_gemm_f8_workspace(-1, 4, 4), lambda: A.fo_gemm_f8_workspace(4, 0, 4),
+                                  lambda: A.fo_gemm_f8_workspace(4, 4, 0), lambda: A.fo_logp_workspace(-1, 4),
+                                  lambda: A.fo_logp_workspace(4, 0)])
+def test_workspace_refuses(call):
+    with pytest.raises(A.FoError):
+        call()
+
+
+# ------------------------------------------------------------------ the binding
+class _Gpu0(torch.Tensor):
+    def get_device(self):
+        return 0
+
+
+class _Gpu1(torch.Tensor):
+    def get_device(self):
+        return 1
+
+
+class _Recorder:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append(name) or A.FO_OK
+
+
+STREAM = types.SimpleNamespace(cuda_stream=0, device_index=0)
+TENSORS = {  # the binding's calls: tensors by name, then the other arguments
+    A.fo_embed_fwd: (dict(tokens=(I32, 4), table=(BF16, 5, 8), out=(BF16, 4, 8)), {}),
+    A.fo_embed_bwd: (dict(tokens=(I32, 4), dout=(BF16, 4, 8), dtable=(BF16, 5, 8), workspace=(U8, 1 << 20)), {}),
+    A.fo_rmsnorm_fwd: (dict(x=(F32, 4, 8), w=(F32, 8), y=(F32, 4, 8), rstd=(F32, 4), residual=(F32, 4, 8), h=(F32, 4, 8)),
+                       dict(eps=1e-6)),
+    A.fo_rmsnorm_bwd: (dict(dy=(BF16, 4, 8), h=(BF16, 4, 8), w=(BF16, 8), rstd=(F32, 4), dx=(BF16, 4, 8), dw=(BF16, 8),
+                            dres=(BF16, 4, 8), workspace=(U8, 1 << 20)), {}),
+    A.fo_rmsnorm_f8: (dict(x=(F32, 4, 8), w=(F32, 8), y8=(F8, 4, 8), y_scale=(F32, 4), residual=(F32, 4, 8), h=(F32, 4, 8)),
+                      dict(eps=1e-6)),
+    A.fo_quant_f8: (dict(x=(F32, 4, 8), y8=(U8, 4, 8), y_scale=(F32, 4)), {}),
+    A.fo_gemm_f8: (dict(a=(F8, 4, 16), a_scale=(F32, 4), b=(F8, 8, 16), b_scale=(F32, 8), c=(BF16, 4, 8),
+                        workspace=(U8, 1 << 20)), {}),
+    A.fo_logp_fwd: (dict(logits=(BF16, 4, 8), targets=(I32, 4), logp=(F32, 4), lse=(F32, 4), workspace=(U8, 64)), {}),
+    A.fo_logp_bwd: (dict(logits=(BF16, 4, 8), targets=(I32, 4), logp=(F32, 4), lse=(F32, 4), dlogp=(F32, 4),
+                         dlogits=(BF16, 4, 8)), {}),
+    A.fo_xent: (dict(logits=(F32, 4, 8), targets=(I32, 4), weight=(F32, 4), loss=(F32, 4), dlogits=(F32, 4, 8),
+                     workspace=(U8, 64)), {}),
+    A.fo_pref_loss: (dict(logp=(F32, 9), ref=(F32, 9), begin=(I32, 4), end=(I32, 4), loss=(F32, 2), reward=(F32, 4),
+                          dlogp=(F32, 9)), {}),
+}
+
+
+def _make(spec):
+    return torch.zeros(spec[1:], dtype=spec[0]).as_subclass(_Gpu0)
+
+
+@pytest.fixture
+def library(monkeypatch):
+    rec = _Recorder()
+    monkeypatch.setattr(A, "_lib", rec)
+    return rec
+
+
+@pytest.mark.parametrize("f", TENSORS, ids=lambda f: f.__name__)
+def test_binding(f, library):
+    """What fits goes through; a tensor of another type, shape, device or spread is refused before the library is
+    called, and so is a stream of another device."""
+    spec, rest = TENSORS[f]
+    good = {n: _make(s) for n, s in spec.items()}
+    f(**good, **rest, stream=STREAM)
+    assert library.calls == [f.__name__]
+
+    def refused(**kw):
+        with pytest.raises(A.FoError):
+            f(**{**good, **rest, "stream": STREAM, **kw})
+
+    for n, s in spec.items():
+        if n != "workspace":
+            refused(**{n: _make((torch.float16 if s[0] in (BF16, F32) else torch.int16,) + s[1:])})
+            if (f, n) != (A.fo_logp_fwd, "logits"):  # any width is a vocabulary
+                refused(**{n: _make(s[:-1] + (s[-1] + 1,))})
+            refused(**{n: _make(s[:-1] + (2 * s[-1],))[..., ::2]})
+        else:
+            refused(**{n: torch.zeros(1, dtype=U8).expand(1 << 20).as_subclass(_Gpu0)})
+        refused(**{n: good[n].as_subclass(_Gpu1)})
+        if len(s) == 3:
+            if (f, n) not in ((A.fo_embed_fwd, "table"), (A.fo_embed_bwd, "dtable")):
+                refused(**{n: _make((s[0], s[1] + 1, s[2]))})
+            refused(**{n: _make((s[0], 1) + s[1:])})
+    refused(stream=types.SimpleNamespace(cuda_stream=0, device_index=1))
+    with pytest.raises(A.FoError):
+        f(**{n: torch.zeros(s[1:], dtype=s[0]) for n, s in spec.items()}, **rest, stream=STREAM)
+    assert library.calls == [f.__name__]
