@@ -157,14 +157,14 @@ FO_API fo_status fo_dropout_bwd(int32_t dtype, int64_t rows, int32_t cols, const
 /* ------------------------------------------------------------------ embedding
  * out_r = scale table[tokens[r]] over rows of `cols` elements; a token outside
  * [0, vocab) (padding) has a row of zeros and takes part in no gradient.  tokens:
- * device int32[rows].  ld: row strides in elements, >= cols.  The product is
+ * device int32[rows].  ld: row strides in elements, >= cols.  cols up to 2^23.  The product is
  * rounded once.  Errors: FO_EINVAL, FO_EHIP. */
 FO_API fo_status fo_embed_fwd(int32_t dtype, int64_t rows, int32_t cols, int32_t vocab, const int32_t* tokens,
                               const void* table, int64_t table_ld, float scale, void* out, int64_t out_ld,
                               void* hip_stream);
 
-/* dtable_v = scale * the sum of dout's rows of token v, in the order of the rows;
- * every row of dtable is written (0 for tokens that do not come).  accumulate !=
+/* dtable_v = scale * the sum of dout's rows of token v; every row of dtable is
+ * written (0 for tokens that do not come).  accumulate !=
  * 0 adds to what dtable holds instead (a table that is the output's weights too)
  * and leaves the rows of other tokens as they are.  Sums are fp32 and rounded
  * once, after that addition.  rows up to 2^28. */

@@ -61,9 +61,14 @@ fo_status check_workspace(const char* what, const void* ws, int64_t bytes, int64
     } while (0)
 
 // ------------------------------------------------------------------ embedding
+// 256 columns a workgroup in a launch's third dimension; 4096 rows a tile of the sort.
+constexpr int32_t kMaxEmbedCols = 1 << 23;
+constexpr int64_t kMaxEmbedRows = int64_t(1) << 28;
+
 static fo_status check_embed(const char* what, int32_t dtype, int64_t rows, int32_t cols, int32_t vocab,
                              const int32_t* tokens, float scale) {
     FO_TRY(check_sizes(what, dtype, rows, cols));
+    FO_CHECK(cols <= kMaxEmbedCols, "%s: %d columns", what, cols);
     FO_CHECK(vocab >= 1 && vocab <= (1 << 30), "%s: vocab=%d", what, vocab);
     FO_CHECK(std::isfinite(scale), "%s: scale=%g", what, scale);
     return check_vector(what, "tokens", tokens, rows, 4, false);
@@ -87,10 +92,8 @@ extern "C" fo_status fo_embed_fwd(int32_t dtype, int64_t rows, int32_t cols, int
     return launch_embed_fwd(dtype, a, (hipStream_t)hip_stream);
 }
 
-constexpr int64_t kMaxEmbedRows = int64_t(1) << 28;
-
 extern "C" int64_t fo_embed_workspace(int64_t rows, int32_t cols, int32_t vocab) {
-    if (rows < 0 || rows > kMaxEmbedRows || cols < 1 || cols > (1 << 30) || vocab < 1 || vocab > (1 << 30)) {
+    if (rows < 0 || rows > kMaxEmbedRows || cols < 1 || cols > kMaxEmbedCols || vocab < 1 || vocab > (1 << 30)) {
         set_error("fo_embed_workspace: %lld rows of %d, vocab=%d", (long long)rows, cols, vocab);
         return -1;
     }
