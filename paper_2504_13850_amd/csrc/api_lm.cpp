@@ -224,6 +224,8 @@ extern "C" fo_status fo_gemm_f8(int32_t dtype, int64_t M, int32_t N, int32_t K, 
     FO_TRY(check_rows(what, "c", c, ldc, M, N, elem_size(dtype), false));
     FO_TRY(check_vector(what, "a_scale", a_scale, M, 4, true));
     FO_TRY(check_vector(what, "b_scale", b_scale, N, 4, true));
+    FO_CHECK(cdiv(M, 256) * cdiv(N, 256) <= 1 << 22, "%s: more workgroups than a launch holds (%lld x %d)", what,
+             (long long)M, N);
     FO_CHECK(!c || (c != (const void*)a && c != (const void*)b), "%s: c is an operand", what);
     FO_TRY(check_workspace(what, workspace, workspace_bytes, gemm_f8_workspace(M, N, K)));
     if (M == 0) return FO_OK;
