@@ -1,4 +1,6 @@
 // Products of 8-bit rows with a scale each: c_mn = a_scale[m] b_scale[n] sum_k a_mk b_nk.
+#include <algorithm>
+
 #include "lm.h"
 #include "row8.h"
 
@@ -134,15 +136,20 @@ __global__ void __launch_bounds__(256) gemm_f8_any_kernel(GemmF8Args g) {
 // Rows that start 16-byte aligned, K a multiple of 16.  BM x BN of c a workgroup, WM x WN waves; 128 of k a step, in
 // two stages of LDS that the copies fill without registers (lane l of a wave writes 16 bytes at the instruction's
 // base + 16 l, so an instruction fills eight rows of 128 bytes).  Chunk c of row r lies at c ^ r % 8 ^ r / 8 % 8: eight
-// neighbouring rows, and sixteen, read one chunk from distinct banks.  The stages are arrays of their own, so that the
-// compiler knows a read of one from a copy into the other.
-__device__ __forceinline__ void copy16(const uint8_t* base, uint32_t off, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds(base + off, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// neighbouring rows, and sixteen, read one chunk from distinct banks.
+// As the compiler's own instruction the copy would be waited for before every read of LDS that it might write; here the
+// kernel's waits alone count: each names the copies that the next step reads.  m0 is free: nothing else here uses it.
+__device__ __forceinline__ uint32_t lds_at(const uint8_t* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
+}
+__device__ __forceinline__ void copy16(const uint8_t* base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
 
-// No copy or LDS operation in flight; and a barrier that, unlike __syncthreads, does not wait for copies.
+// At most N copies and no LDS operation in flight, and a barrier: unlike __syncthreads it does not wait for all copies.
+template <int N>
 __device__ __forceinline__ void stage_barrier() {
-    __builtin_amdgcn_s_waitcnt(7 << 4);
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -150,12 +157,14 @@ __device__ __forceinline__ void stage_barrier() {
 
 constexpr int64_t kTileStride = int64_t(1) << 23;  // 256 rows have 32-bit offsets
 
-template <class T, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g, int tiles_m, int tiles_n) {
+// T: the type that chooses the arithmetic; Out: that of the elements of c, T or, for a slice of k, float.
+template <class T, class Out, int BM, int BN, int WM, int WN, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g, int tiles_m, int tiles_n, int slice) {
     constexpr int WAVES = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, CA = BM / 8 / WAVES, CB = BN / 8 / WAVES;
     static_assert(BM % (WM * 32) == 0 && BN % (WN * 32) == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "tiles");
-    __shared__ __align__(1024) uint8_t st0[(BM + BN) * 128];
-    __shared__ __align__(1024) uint8_t st1[(BM + BN) * 128];
+    __shared__ __align__(1024) uint8_t st0[(BM + BN) * 128], st1[(BM + BN) * 128];
+    __shared__ __align__(1024) uint8_t st2[STAGES > 2 ? (BM + BN) * 128 : 16], st3[STAGES > 3 ? (BM + BN) * 128 : 16];
+    uint8_t* const stage[4] = {st0, st1, st2, st3};
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // workgroups go to the eight XCDs in turn: each takes a run of tiles, in columns of eight tiles, so that tiles
     // that share rows of a or b share an L2
@@ -168,7 +177,9 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
 
     // this lane's part of a copy: row lane / 8 of eight, the chunk that belongs at lane % 8; rows past the last are the
     // last one again, their results are not stored
-    const uint8_t *a = g.a + m0 * g.lda, *b = g.b + (int64_t)n0 * g.ldb;
+    const int64_t k0 = (int64_t)blockIdx.y * slice;  // the slice of k: a multiple of 128, all of it in one
+    const int K = (int)min((int64_t)slice, g.K - k0);
+    const uint8_t *a = g.a + m0 * g.lda + k0, *b = g.b + (int64_t)n0 * g.ldb + k0;
     const int last_a = (int)min(g.M - m0, (int64_t)BM) - 1, last_b = min(g.N - n0, BN) - 1;
     uint32_t off_a[CA], off_b[CB];
     const auto chunk = [&](int q) { return ((lane & 7) ^ (lane >> 3) ^ (q & 7)) * 16; };
@@ -179,10 +190,11 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
     for (int i = 0; i < CB; ++i)
         off_b[i] = (uint32_t)(min((wave + i * WAVES) * 8 + (lane >> 3), last_b) * (int)g.ldb + chunk(BM / 8 + wave + i * WAVES));
     const auto copy = [&](uint8_t* st, int64_t k) {
+        const uint32_t to = lds_at(st) + wave * 1024;
 #pragma unroll
-        for (int i = 0; i < CA; ++i) copy16(a + k, off_a[i], st + (wave + i * WAVES) * 1024);
+        for (int i = 0; i < CA; ++i) copy16(a + k, off_a[i], to + i * WAVES * 1024);
 #pragma unroll
-        for (int i = 0; i < CB; ++i) copy16(b + k, off_b[i], st + (BM / 8 + wave + i * WAVES) * 1024);
+        for (int i = 0; i < CB; ++i) copy16(b + k, off_b[i], to + (BM / 8 + i * WAVES) * 1024);
     };
 
     f32x16 acc[TN][TM] = {};
@@ -212,28 +224,24 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
             }
         }
     };
-    const int steps = g.K / 128;
+    // a copy is issued STAGES - 1 steps ahead, also past the last (that one again), so that their number is known
+    constexpr int AHEAD = STAGES - 1;
+    const int steps = K / 128;
     if (steps) {
-        copy(st0, 0);
-        stage_barrier();
-        int t = 0;
-        for (; t + 2 < steps; t += 2) {
-            copy(st1, (int64_t)(t + 1) * 128);
-            compute(st0);
-            stage_barrier();  // st1 is here, and st0 has been read
-            copy(st0, (int64_t)(t + 2) * 128);
-            compute(st1);
-            stage_barrier();
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) copy(stage[u], (int64_t)min(u, steps - 1) * 128);
+        for (int t = 0; t < steps; t += STAGES) {
+#pragma unroll
+            for (int u = 0; u < STAGES; ++u) {
+                if (t + u >= steps) break;
+                stage_barrier<(CA + CB) * (AHEAD - 1)>();  // this step's stage is here, and the one before has been read
+                copy(stage[(u + AHEAD) % STAGES], (int64_t)min(t + u + AHEAD, steps - 1) * 128);
+                compute(stage[u]);
+            }
         }
-        if (t + 1 < steps) copy(st1, (int64_t)(t + 1) * 128);
-        compute(st0);
-        stage_barrier();
-        if (t + 1 < steps) {
-            compute(st1);
-            stage_barrier();
-        }
+        stage_barrier<0>();
     }
-    if (const int rest = g.K % 128) {  // chunks past K are zeros
+    if (const int rest = K % 128) {  // chunks past K are zeros
         const int64_t k = (int64_t)steps * 128;
 #pragma unroll
         for (int i = 0; i < CA + CB; ++i) {
@@ -242,17 +250,18 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
             if (chunk(q) < rest) v = *(const i32x4*)((i < CA ? a + off_a[i < CA ? i : 0] : b + off_b[i < CA ? 0 : i - CA]) + k);
             *(i32x4*)(st0 + q * 1024 + lane * 16) = v;
         }
-        stage_barrier();
+        stage_barrier<0>();
         compute(st0);
-        stage_barrier();
+        stage_barrier<0>();
     }
 
     // 32 rows of the wave at a time through its part of the LDS, so that rows are written 16 bytes a lane: straight from
-    // the accumulators, which hold four columns of 32 rows, 8192^3 took TIME_STRAIGHT us
-    constexpr int E = 16 / sizeof(T), ROW = TN * 32 / E;  // elements of a chunk, chunks of a row
-    uint8_t* mine = st0 + wave * (32 * TN * 32 * (int)sizeof(T));
-    static_assert(WAVES * 32 * TN * 32 * sizeof(T) <= sizeof(st0), "the waves' rows fit a stage");
+    // the accumulators, which hold four columns of 32 rows, 8192^3 took 462 us and not 431
+    constexpr int E = 16 / sizeof(Out), ROW = TN * 32 / E;  // elements of a chunk, chunks of a row
+    uint8_t* mine = st0 + wave * (32 * TN * 32 * (int)sizeof(Out));
+    static_assert(WAVES * 32 * TN * 32 * sizeof(Out) <= sizeof(st0), "the waves' rows fit a stage");
     const int nw = n0 + wn - BM;
+    Out* c = (Out*)g.c + blockIdx.y * g.M * g.ldc;
     float sb[TN][16];
 #pragma unroll
     for (int j = 0; j < TN; ++j)
@@ -267,23 +276,23 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                T v[4];
+                Out v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = from_f<T>(acc[j][i][q * 4 + e] * sa * sb[j][q * 4 + e]);
-                const int n = j * 32 + q * 8 + (lane >> 5) * 4, c = n / E;
-                __builtin_memcpy(mine + ((lane & 31) * ROW + (c ^ (lane & (ROW - 1)))) * 16 + n % E * sizeof(T), v, sizeof(v));
+                for (int e = 0; e < 4; ++e) v[e] = from_f<Out>(acc[j][i][q * 4 + e] * sa * sb[j][q * 4 + e]);
+                const int n = j * 32 + q * 8 + (lane >> 5) * 4, x = n / E;
+                __builtin_memcpy(mine + ((lane & 31) * ROW + (x ^ (lane & (ROW - 1)))) * 16 + n % E * sizeof(Out), v, sizeof(v));
             }
         __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll
         for (int x = lane; x < 32 * ROW; x += 64) {
-            const int r = x / ROW, c = x % ROW, n = nw + c * E;
-            const u32x4 u = *(const u32x4*)(mine + (r * ROW + (c ^ (r & (ROW - 1)))) * 16);
+            const int r = x / ROW, q = x % ROW, n = nw + q * E;
+            const u32x4 u = *(const u32x4*)(mine + (r * ROW + (q ^ (r & (ROW - 1)))) * 16);
             if (mw + r >= g.M) continue;
-            T* p = (T*)g.c + (mw + r) * g.ldc + n;
+            Out* p = c + (mw + r) * g.ldc + n;
             if (n + E <= g.N) {
                 *(u32x4_any*)p = u;
             } else {
-                T v[E];
+                Out v[E];
                 __builtin_memcpy(v, &u, 16);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
@@ -294,32 +303,159 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
     }
 }
 
-template <class T, int BM, int BN, int WM, int WN>
-void launch_tiles(const GemmF8Args& g, hipStream_t s) {
-    const int tm = (int)cdiv(g.M, BM), tn = (int)cdiv(g.N, BN);
-    gemm_f8_tile_kernel<T, BM, BN, WM, WN><<<(unsigned)(cdiv((int64_t)tm * tn, 8) * 8), 64 * WM * WN, 0, s>>>(g, tm, tn);
+// ------------------------------------------------------------------ few rows of a
+// Up to 32 rows: b is read once, straight into registers; 16 columns a workgroup, whose waves take runs of k and join
+// their sums in order.  b's rows are the matrix instruction's first operand, a's 16 TM rows its second.
+template <class T, int TM, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) gemm_f8_few_kernel(GemmF8Args g) {
+    constexpr int FLY = TM == 1 ? 8 : 4;  // steps of 128 in flight
+    __shared__ f32x4 part[WAVES][TM][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)block_of() * 16;
+    if (n0 >= g.N) return;
+    const int steps = (g.K + 127) / 128, each = (steps + WAVES - 1) / WAVES;
+    const int first = min(steps, wave * each), last = min(steps, first + each);
+    const uint8_t* b = g.b + min(n0 + (lane & 15), (int64_t)g.N - 1) * g.ldb + (lane >> 4) * 32;
+    const uint8_t* a[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) a[i] = g.a + min((int64_t)(i * 16 + (lane & 15)), g.M - 1) * g.lda + (lane >> 4) * 32;
+    const auto load = [&](const uint8_t* p, int t) {  // chunks past K are zeros
+        const int k = t * 128 + (lane >> 4) * 32;
+        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        if (k < g.K) lo = *(const i32x4*)(p + (int64_t)t * 128);
+        if (k + 16 < g.K) hi = *(const i32x4*)(p + (int64_t)t * 128 + 16);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    f32x4 acc[TM] = {};
+    for (int t = first; t < last; t += FLY) {
+        i32x8 vb[FLY], va[FLY][TM];
+#pragma unroll
+        for (int u = 0; u < FLY; ++u)
+            if (t + u < last) {
+                vb[u] = load(b, t + u);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) va[u][i] = load(a[i], t + u);
+            }
+#pragma unroll
+        for (int u = 0; u < FLY; ++u)
+            if (t + u < last) {
+                const Frag<T> fb(vb[u]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) acc[i] = mma(fb, Frag<T>(va[u][i]), acc[i]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= TM) return;
+    f32x4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += part[w][wave][lane];
+    const int64_t m = wave * 16 + (lane & 15);
+    const int n = (int)n0 + (lane >> 4) * 4;
+    if (m >= g.M || n >= g.N) return;
+    const float sa = g.a_scale ? g.a_scale[m] : 1.f;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = sum[e] * sa * (g.b_scale && n + e < g.N ? g.b_scale[n + e] : 1.f);
+    store4<T>(g, m, n, v);
+}
+
+// ------------------------------------------------------------------ the launches
+// c from the slices' sums, [slices][M][N], in order.  A thread has four columns.
+template <class T>
+__global__ void __launch_bounds__(256) gemm_f8_join_kernel(GemmF8Args g, const float* __restrict__ part, int slices) {
+    const int64_t quads = (g.N + 3) / 4, id = (int64_t)block_of() * 256 + threadIdx.x, m = id / quads;
+    if (m >= g.M) return;
+    const int n = (int)(id - m * quads) * 4;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int at = min(n + e, g.N - 1);
+        float sum = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < slices; ++k) sum += part[(k * g.M + m) * g.N + at];
+        v[e] = sum * (g.a_scale ? g.a_scale[m] : 1.f) * (g.b_scale ? g.b_scale[at] : 1.f);
+    }
+    store4<T>(g, m, n, v);
+}
+
+// Which kernel, by what each took (us) on one card:
+//   M     N      K      few rows  64 x 64  128 x 128, 3 stages  2 stages  256 x 256
+//   4     4096   4096   6.5       17.5
+//   1     128000 4096   88        99
+//   20    128000 1024   47        24
+//   32    4096   4096   9.5       17.5
+//   256   4096   4096             10.9     20.6                 23.9      43.9
+//   1024  4096   4096             30       23.7                 27.1      47.2
+//   2603  2304   768              16.3     16.3                 12.2      17.2
+//   2048  4096   4096             56       44.8                 35.1      50.7
+//   4096  4096   4096             104      86                   65.7      60.1
+//   8192  8192   8192             858      629                  521       431
+// Tiles of 64 hold four stages and of 128 three where a CU has a workgroup or two at a time: the copies then have the
+// memory's latency for themselves.  From two rounds of workgroups on, two stages and two workgroups a CU hide it better.
+constexpr int kCUs = 256;
+bool few_rows(const GemmF8Args& g) { return g.M <= 16 || (g.M <= 32 && cdiv(g.N, 64) < kCUs); }
+// Slices of k, of 2048 or more, where 64 x 64 tiles are few and k is long: 100 x 1024 x 8192 14.2 -> 11.8 us, 40 x 512 x
+// 16384 23.6 -> 10.9; the launch that joins them eats the gain up where k is shorter (256 x 256 x 4096 9.2 -> 9.9).
+int slices_of(int64_t M, int32_t N, int32_t K) {
+    const int64_t tiles = cdiv(M, 64) * cdiv(N, 64);
+    return tiles > kCUs / 4 || K < 8192 ? 1 : std::min(K / 2048, 16);
+}
+
+template <class T, class Out, int BM, int BN, int WM, int WN, int STAGES>
+void launch_tiles(const GemmF8Args& g, int slices, hipStream_t s) {
+    const int tm = (int)cdiv(g.M, BM), tn = (int)cdiv(g.N, BN), slice = (int)(cdiv(cdiv(g.K, 128), slices) * 128);
+    const dim3 grid((unsigned)(cdiv((int64_t)tm * tn, 8) * 8), (unsigned)cdiv(g.K, slice));
+    gemm_f8_tile_kernel<T, Out, BM, BN, WM, WN, STAGES><<<grid, 64 * WM * WN, 0, s>>>(g, tm, tn, slice);
 }
 
 template <class T>
-fo_status run(const GemmF8Args& g, hipStream_t s) {
-    const bool whole = g.K % 16 == 0 && g.lda < kTileStride && g.ldb < kTileStride && g.lda % 16 == 0 && g.ldb % 16 == 0 && ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0;
-#ifndef SHAPE
-#define SHAPE 0
-#endif
-    if (!whole) gemm_f8_any_kernel<T><<<grid_of(cdiv(g.M, 64) * cdiv(g.N, 64)), 256, 0, s>>>(g);
-    else if (SHAPE == 1 || (SHAPE == 0 && cdiv(g.M, 256) * cdiv(g.N, 256) >= 256)) launch_tiles<T, 256, 256, 2, 4>(g, s);
-    else if (SHAPE == 2 || (SHAPE == 0 && cdiv(g.M, 128) * cdiv(g.N, 128) >= 256)) launch_tiles<T, 128, 128, 2, 2>(g, s);
-    else launch_tiles<T, 64, 64, 2, 2>(g, s);
+fo_status run(const GemmF8Args& g, float* part, hipStream_t s) {
+    const bool whole = g.K % 16 == 0 && g.lda < kTileStride && g.ldb < kTileStride && g.lda % 16 == 0 &&
+                       g.ldb % 16 == 0 && ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0;
+    const auto tiles = [&](int side) { return cdiv(g.M, side) * cdiv(g.N, side); };
+    const int slices = slices_of(g.M, g.N, g.K);
+    if (!whole) {
+        gemm_f8_any_kernel<T><<<grid_of(tiles(64)), 256, 0, s>>>(g);
+    } else if (few_rows(g)) {
+        const dim3 grid = grid_of(cdiv(g.N, 16));
+        // eight waves share k where columns are few (4 x 4096 x 4096: 6.5 us either way), else four (1 x 128000 x 4096:
+        // 88 us, 108 with eight)
+        if (g.M > 16) gemm_f8_few_kernel<T, 2, 8><<<grid, 512, 0, s>>>(g);
+        else if (g.N < 16 * 4 * kCUs) gemm_f8_few_kernel<T, 1, 8><<<grid, 512, 0, s>>>(g);
+        else gemm_f8_few_kernel<T, 1, 4><<<grid, 256, 0, s>>>(g);
+    } else if (slices > 1) {
+        GemmF8Args h = g;
+        h.c = part;
+        h.ldc = g.N;
+        h.a_scale = h.b_scale = nullptr;
+        launch_tiles<T, float, 64, 64, 2, 2, 4>(h, slices, s);
+        FO_LAUNCHED();
+        const int n = (int)cdiv(g.K, cdiv(cdiv(g.K, 128), slices) * 128);
+        gemm_f8_join_kernel<T><<<grid_of(cdiv(g.M * cdiv(g.N, 4), 256)), 256, 0, s>>>(g, part, n);
+    } else if (tiles(64) <= 2 * kCUs) {
+        launch_tiles<T, T, 64, 64, 2, 2, 4>(g, 1, s);
+    } else if (tiles(128) <= kCUs) {
+        launch_tiles<T, T, 128, 128, 2, 2, 3>(g, 1, s);
+    } else if (tiles(256) < kCUs * 3 / 4) {
+        launch_tiles<T, T, 128, 128, 2, 2, 2>(g, 1, s);
+    } else {
+        launch_tiles<T, T, 256, 256, 2, 4, 2>(g, 1, s);
+    }
     FO_LAUNCHED();
     return FO_OK;
 }
 
 }  // namespace
 
-int64_t gemm_f8_workspace(int64_t M, int32_t N, int32_t K) { return 0; }
+int64_t gemm_f8_workspace(int64_t M, int32_t N, int32_t K) {
+    const int slices = M ? slices_of(M, N, K) : 1;
+    return slices > 1 ? cdiv((int64_t)slices * M * N * 4, 16) * 16 : 0;
+}
 
 fo_status launch_gemm_f8(int32_t dtype, const GemmF8Args& g, void* ws, hipStream_t s) {
-    return dtype == FO_DT_BF16 ? run<bf16_t>(g, s) : run<float>(g, s);
+    return dtype == FO_DT_BF16 ? run<bf16_t>(g, (float*)ws, s) : run<float>(g, (float*)ws, s);
 }
 
 }  // namespace fo

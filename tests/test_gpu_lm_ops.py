@@ -277,7 +277,8 @@ def test_f8_rounding():
 # ------------------------------------------------------------------ 8-bit product
 GEMM = [(1, 1, 1), (1, 5, 16), (3, 64, 128), (7, 100, 77), (16, 16, 4096), (1, 4096, 512), (5, 130, 2064), (33, 257, 384),
         (64, 512, 1024), (65, 300, 100), (130, 129, 640), (257, 640, 256), (300, 1000, 1500), (520, 513, 2048),
-        (1030, 768, 912), (2, 20, 9001)]
+        (1030, 768, 912), (2, 20, 9001),
+        (40, 100, 8208), (70, 130, 16400), (130, 64, 12304), (20, 17000, 160), (700, 4100, 272), (2049, 2600, 400), (3400, 3500, 160)]
 
 
 def _bytes(seed, rows, cols):
