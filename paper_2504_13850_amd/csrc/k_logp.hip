@@ -13,69 +13,83 @@ namespace fo {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+constexpr float kLeast = -3.402823466e38f;
 
-// Maximum and sum of exp(z - maximum) over some terms, by raw logits: z = scale raw, scale > 0.
+// Maximum and sum of exp(scale (raw - maximum)) over some terms by their raw logits.  The maximum starts from the least
+// finite number and not from -infinity, so that no difference of infinities arises: a sum of 0 has no terms, or none
+// but -infinity.  A NaN goes by the maximum and into the sum.  c = scale log2(e).
 struct Part {
     float m, s;
 };
-// exp(scale raw - scale m) where m may be -infinity (no term, or none but -infinity).
-__device__ __forceinline__ float term(float raw, float scale, float m) {
-    return exp_(m == -INFINITY ? -INFINITY : (raw - m) * scale);
-}
-__device__ __forceinline__ Part join(Part a, Part b, float scale) {
+constexpr Part kNone = {kLeast, 0.f};
+__device__ __forceinline__ float term(float raw, float m, float c) { return __builtin_amdgcn_exp2f((raw - m) * c); }
+__device__ __forceinline__ Part join(Part a, Part b, float c) {
     const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) return {m, a.s + b.s};  // 0, or NaN
-    return {m, a.s * exp_((a.m - m) * scale) + b.s * exp_((b.m - m) * scale)};
+    return {m, a.s * term(a.m, m, c) + b.s * term(b.m, m, c)};
 }
 template <int TPR>
-__device__ __forceinline__ Part team_join(Part p, float scale, Part* lds) {
+__device__ __forceinline__ Part team_join(Part p, float c, Part* lds) {
 #pragma unroll
     for (int m = 1; m < (TPR < 64 ? TPR : 64); m *= 2)
-        p = join(p, Part{__shfl_xor(p.m, m), __shfl_xor(p.s, m)}, scale);
+        p = join(p, Part{__shfl_xor(p.m, m), __shfl_xor(p.s, m)}, c);
     if constexpr (TPR > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = p;
         __syncthreads();
         p = lds[threadIdx.x & (TPR / 64 - 1)];
 #pragma unroll
-        for (int m = 1; m < TPR / 64; m *= 2) p = join(p, Part{__shfl_xor(p.m, m), __shfl_xor(p.s, m)}, scale);
+        for (int m = 1; m < TPR / 64; m *= 2) p = join(p, Part{__shfl_xor(p.m, m), __shfl_xor(p.s, m)}, c);
     }
     return p;
 }
 
-// logp and lse from the other terms and the target's logit; all: what the row's terms are divided by, as {m, 1 / s},
-// and the target's 1 - p.
+// What a row's gradient needs of the other terms and the target's logit zt: the maximum, 1 / the sum of all terms, and
+// the other terms' share, which is the target's 1 - p.
 struct Row {
-    float logp, lse, m, inv, rest;
+    float m, inv, rest;
+    bool none;  // every term is 0
 };
-__device__ __forceinline__ Row row_of(Part p, float zt, float scale) {
+__device__ __forceinline__ Row row_of(Part p, float zt, float c) {
     Row r;
     r.m = fmaxf(p.m, zt);
-    if (p.s != p.s || zt != zt) r.m = NAN;
-    const float others = p.s * term(p.m, scale, r.m), own = term(zt, scale, r.m), all = others + own;
+    const float others = p.s * term(p.m, r.m, c), all = others + term(zt, r.m, c);
+    r.none = all == 0.f;
     r.inv = 1.f / all;
-    r.rest = others * r.inv;
-    r.logp = zt >= p.m ? -log1pf(others) : (zt - r.m) * scale - logf(all);
-    r.lse = r.m * scale + logf(all);
-    if (r.m == -INFINITY) {
-        r.logp = r.lse = -INFINITY;
-        r.rest = 0.f;
-    }
+    r.rest = r.none ? 0.f : others * r.inv;
     return r;
 }
+// logp and lse, in 64 bits: a loss over whole answers adds up what they are off by.
+__device__ __forceinline__ float2 logs_of(Part p, float zt, float scale) {
+    const float c = scale * kLog2e, m = fmaxf(p.m, zt);
+    const double others = (double)p.s * term(p.m, m, c), all = others + term(zt, m, c);
+    if (all == 0.0) return make_float2(-INFINITY, -INFINITY);
+    const double away = ((double)zt - m) * scale;
+    return make_float2((float)(zt >= p.m ? -log1p(others) : away - log(all)), (float)((double)m * scale + log(all)));
+}
 
-// The chunk's sum and maximum, the target's element (place t, if it lies here) left out.
+// -infinity in the target's place, if it lies in this chunk.
 template <class T>
-__device__ __forceinline__ void add_chunk(const Eight<T, false>& x, int n, int t, float scale, Part& p) {
-    float v[8], m = p.m;
+__device__ __forceinline__ void leave_out(Eight<T, false>& x, int chunk, int target) {
+    if (target >> 3 == chunk) x.put(target & 7, from_f<T>(-INFINITY));
+}
+// What a row has past its last whole chunk, -infinity after it.
+template <class T>
+__device__ __forceinline__ Eight<T, false> last_chunk(const T* row, int vocab) {
+    const int c0 = vocab & ~7, n = vocab & 7;
+    Eight<T, false> x;
+    x.load(row + c0, n, false);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        v[e] = e < n && e != t ? x.at(e) : -INFINITY;
-        m = fmaxf(m, v[e]);
-    }
-    float s = p.s * term(p.m, scale, m);
+    for (int e = 0; e < 8; ++e)
+        if (e >= n) x.put(e, from_f<T>(-INFINITY));
+    return x;
+}
+template <class T>
+__device__ __forceinline__ void add_chunk(const Eight<T, false>& x, float c, Part& p) {
+    float m = p.m;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += v[e] != v[e] ? v[e] : term(v[e], scale, m);
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, x.at(e));
+    float s = p.s * term(p.m, m, c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += term(x.at(e), m, c);
     p = {m, s};
 }
 
@@ -91,35 +105,45 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) logp_fwd_kernel(LogpArg
     if (row >= a.rows) return;
     const int target = a.targets[row];
     const bool there = target >= 0 && target < a.vocab;
-    Part p = {-INFINITY, 0.f};
+    const float c2 = a.scale * kLog2e;
+    Part p = kNone;
     if (there) {
         const T* x = (const T*)a.logits + row * a.ld;
-        const int chunks = (a.vocab + 7) / 8, each = SLICED ? (chunks + slices - 1) / slices : chunks;
-        const int first = SLICED ? (int)(id % slices) * each : 0, last = min(chunks, first + each);
-        for (int c = first + t; c < last; c += FLY * TPR) {
+        const int chunks = a.vocab / 8, each = SLICED ? (chunks + slices - 1) / slices : chunks;
+        const int slice = SLICED ? (int)(id % slices) : 0, first = min(chunks, slice * each), last = min(chunks, first + each);
+        int c = first + t;
+        for (; c + (FLY - 1) * TPR < last; c += FLY * TPR) {  // the loads first, without a branch between them
             Eight<T, false> u[FLY];
 #pragma unroll
-            for (int k = 0; k < FLY; ++k) {
-                const int c0 = (c + k * TPR) * 8, n = min(8, a.vocab - c0);
-                if (c + k * TPR < last) u[k].load(x + c0, n, n == 8);
-            }
+            for (int k = 0; k < FLY; ++k) u[k].load(x + (c + k * TPR) * 8, 8, true);
 #pragma unroll
             for (int k = 0; k < FLY; ++k) {
-                const int c0 = (c + k * TPR) * 8;
-                if (c + k * TPR < last) add_chunk(u[k], a.vocab - c0, target - c0, a.scale, p);
+                leave_out(u[k], c + k * TPR, target);
+                add_chunk(u[k], c2, p);
             }
         }
-        p = team_join<TPR>(p, a.scale, lds);
+        for (; c < last; c += TPR) {
+            Eight<T, false> u;
+            u.load(x + c * 8, 8, true);
+            leave_out(u, c, target);
+            add_chunk(u, c2, p);
+        }
+        if (a.vocab % 8 && t == 0 && slice == slices - 1) {
+            Eight<T, false> u = last_chunk(x, a.vocab);
+            leave_out(u, chunks, target);
+            add_chunk(u, c2, p);
+        }
+        p = team_join<TPR>(p, c2, lds);
     }
     if (t) return;
     if (SLICED) {
         part[id] = p;
         return;
     }
-    Row r = {};
-    if (there) r = row_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
-    a.logp[row] = r.logp;
-    if (a.lse) a.lse[row] = r.lse;
+    float2 r = make_float2(0.f, 0.f);
+    if (there) r = logs_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
+    a.logp[row] = r.x;
+    if (a.lse) a.lse[row] = r.y;
 }
 
 // A wave a row: the slices in order of their lanes.
@@ -128,20 +152,21 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
     const int64_t row = block_of();
     if (row >= a.rows) return;
     const int target = a.targets[row];
-    Row r = {};
+    float2 r = make_float2(0.f, 0.f);
     if (target >= 0 && target < a.vocab) {
-        Part p = {-INFINITY, 0.f};
-        for (int k = threadIdx.x; k < slices; k += 64) p = join(p, part[row * slices + k], a.scale);
-        p = team_join<64>(p, a.scale, nullptr);
-        r = row_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
+        const float c = a.scale * kLog2e;
+        Part p = kNone;
+        for (int k = threadIdx.x; k < slices; k += 64) p = join(p, part[row * slices + k], c);
+        p = team_join<64>(p, c, nullptr);
+        r = logs_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
     }
     if (threadIdx.x) return;
-    a.logp[row] = r.logp;
-    if (a.lse) a.lse[row] = r.lse;
+    a.logp[row] = r.x;
+    if (a.lse) a.lse[row] = r.y;
 }
 
-// XENT: weight is minus the gradient by logp, and logp becomes the loss.
-template <class T, bool XENT>
+// XENT: weight is minus the gradient by logp, and logp becomes the loss.  NT: past the caches.
+template <class T, bool XENT, bool NT>
 __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, float* __restrict__ loss) {
     const int64_t row = block_of();
     if (row >= a.rows) return;
@@ -158,21 +183,23 @@ __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, float* __rest
         const int c0 = c * 8, n = min(8, a.vocab - c0);
         float d[8] = {};
         if (!none) {
-            Eight<T, false> u;
+            Eight<T, NT> u;
             u.load(x + c0, n, n == 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = -g * exp_(fmaf(u.at(e), a.scale, -lse));
+                d[e] = -g * __builtin_amdgcn_exp2f(fmaf(u.at(e), a.scale, -lse) * kLog2e);
                 if (c0 + e == target) d[e] = own;
             }
         }
-        Eight<T, false>::store(y + c0, d, n, n == 8);
+        Eight<T, NT>::store(y + c0, d, n, n == 8);
     }
 }
 
-// Cross-entropy with the row in registers: maximum and sum of what is held, then the gradient from it.
-template <class T, int TPR, int NC>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) xent_kernel(LogpArgs a) {
+// Cross-entropy with the row in registers: maximum and sum of what is held, then the gradient from it.  64 registers,
+// two workgroups of 1024 on a CU, where a thread holds four chunks: one works while the other waits (8192 rows of 32000
+// bf16 177 us, 224 with one).  NT: the gradient past the caches.
+template <class T, int TPR, int NC, bool NT>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 4) xent_kernel(LogpArgs a) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, RPW = THREADS / TPR;
     __shared__ float lds[32];
     const int t = threadIdx.x % TPR;
@@ -185,52 +212,47 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) xent_kernel(LogpArgs a)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int c0 = (t + c * TPR) * 8, n = min(8, a.vocab - c0);
-            if (n > 0) Eight<T, false>::store(y + c0, zero, n, n == 8);
+            if (n > 0) Eight<T, NT>::store(y + c0, zero, n, n == 8);
         }
         if (t == 0) a.logp[row] = 0.f;
         return;
     }
     const T* x = (const T*)a.logits + row * a.ld;
     const float zt = to_f(x[target]);
+    const float c2 = a.scale * kLog2e;
+    const int chunks = a.vocab / 8;  // one at least
     Eight<T, false> u[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int c0 = (t + c * TPR) * 8, n = min(8, a.vocab - c0);
-        u[c].load(x + c0, n, n == 8);
+    for (int c = 0; c < NC; ++c) u[c].load(x + min(t + c * TPR, chunks - 1) * 8, 8, true);
+    Part p = kNone;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {  // past the whole chunks: the row's end, or nothing
+        if (t + c * TPR >= chunks) u[c] = last_chunk(x, t + c * TPR == chunks ? a.vocab : 0);
+        leave_out(u[c], t + c * TPR, target);
     }
-    float m = -INFINITY, s = 0.f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int c0 = (t + c * TPR) * 8;
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c0 + e < a.vocab && c0 + e != target) m = fmaxf(m, u[c].at(e));
-    }
-    m = team<TPR>(m, lds, Max());
+        for (int e = 0; e < 8; ++e) p.m = fmaxf(p.m, u[c].at(e));
+    p.m = team<TPR>(p.m, lds, Max());
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int c0 = (t + c * TPR) * 8;
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = u[c].at(e);
-            if (c0 + e < a.vocab && c0 + e != target) s += v != v ? v : term(v, a.scale, m);
-        }
-    }
-    s = team<TPR>(s, lds + 16, Add());  // every thread has read its logits: dlogits may lie over them
-    const Row r = row_of(Part{m, s}, zt, a.scale);
-    const bool none = r.m == -INFINITY;
-    const float g = none ? 0.f : a.weight[row] * a.scale, k = g * r.inv;
-    if (t == 0) a.logp[row] = -r.logp;
+        for (int e = 0; e < 8; ++e) p.s += term(u[c].at(e), p.m, c2);
+    p.s = team<TPR>(p.s, lds + 16, Add());  // every thread has read its logits: dlogits may lie over them
+    const Row r = row_of(p, zt, c2);
+    const float g = r.none ? 0.f : a.weight[row] * a.scale, k = r.none ? 0.f : g * r.inv;
+    if (t == 0) a.logp[row] = -logs_of(p, zt, a.scale).x;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int c0 = (t + c * TPR) * 8, n = min(8, a.vocab - c0);
         float d[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            d[e] = none ? 0.f : k * term(u[c].at(e), a.scale, r.m);
-            if (c0 + e == target) d[e] = -g * r.rest;
-        }
-        if (n > 0) Eight<T, false>::store(y + c0, d, n, n == 8);
+        for (int e = 0; e < 8; ++e) d[e] = k * term(u[c].at(e), r.m, c2);
+        if (target >> 3 == t + c * TPR)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = e == (target & 7) ? -g * r.rest : d[e];
+        if (n > 0) Eight<T, NT>::store(y + c0, d, n, n == 8);
     }
 }
 
@@ -268,39 +290,43 @@ dim3 bwd_grid(const LogpArgs& a) {
     return g;
 }
 
-template <class T>
-fo_status bwd(const LogpArgs& a, hipStream_t s) {
-    logp_bwd_kernel<T, false><<<bwd_grid(a), 256, 0, s>>>(a, nullptr);
+// Logits and gradient that no cache keeps: a step of 5565 rows of 32000 bf16 takes 182 us with the gradient's loads and
+// stores past the caches, 232 through them.
+bool past_caches(const LogpArgs& a, int size) { return 2 * a.rows * a.vocab * size > int64_t(256) << 20; }
+
+template <class T, bool XENT>
+fo_status bwd(const LogpArgs& a, float* loss, hipStream_t s) {
+    if (past_caches(a, sizeof(T))) logp_bwd_kernel<T, XENT, true><<<bwd_grid(a), 256, 0, s>>>(a, loss);
+    else logp_bwd_kernel<T, XENT, false><<<bwd_grid(a), 256, 0, s>>>(a, loss);
     FO_LAUNCHED();
     return FO_OK;
 }
 
-// Rows that a workgroup holds in registers: 8 NC logits a thread.  A few rows longer than one workgroup's share go
-// through the sliced forward pass and the gradient.
-bool held(int64_t rows, int32_t vocab, int32_t size) {
-    return slices_of(rows, vocab) == 1 && (int64_t)vocab * size <= 262144;
+// Rows that a workgroup holds in registers: 8 NC logits a thread, a whole chunk at least.  Longer ones, and a few rows
+// that one workgroup each would be slow for, go through the forward pass and the gradient.
+bool held(int64_t rows, int32_t vocab) { return slices_of(rows, vocab) == 1 && vocab >= 8 && vocab <= 65536; }
+
+template <class T, int TPR, int NC>
+void launch_xent(const LogpArgs& a, hipStream_t s) {
+    constexpr int THREADS = TPR < 256 ? 256 : TPR;
+    const dim3 g = grid_of(cdiv(a.rows, THREADS / TPR));
+    if (past_caches(a, sizeof(T))) xent_kernel<T, TPR, NC, true><<<g, THREADS, 0, s>>>(a);
+    else xent_kernel<T, TPR, NC, false><<<g, THREADS, 0, s>>>(a);
 }
 
 template <class T>
 fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
-    if (!held(a.rows, a.vocab, sizeof(T))) {
+    if (!held(a.rows, a.vocab)) {
         LogpArgs b = a;
         b.logp = (float*)((char*)ws + part_bytes(a.rows, a.vocab));
         b.lse = b.logp + a.rows;
         const fo_status st = fwd<T>(b, ws, s);
-        if (st != FO_OK) return st;
-        logp_bwd_kernel<T, true><<<bwd_grid(b), 256, 0, s>>>(b, a.logp);
-    } else if (a.vocab <= 1024) {
-        xent_kernel<T, 64, 2><<<grid_of(cdiv(a.rows, 4)), 256, 0, s>>>(a);
-    } else if (a.vocab <= 8192) {
-        xent_kernel<T, 256, 4><<<grid_of(a.rows), 256, 0, s>>>(a);
-    } else if (a.vocab <= 32768) {
-        xent_kernel<T, 1024, 4><<<grid_of(a.rows), 1024, 0, s>>>(a);
-    } else if (a.vocab <= 65536) {
-        xent_kernel<T, 1024, 8><<<grid_of(a.rows), 1024, 0, s>>>(a);
-    } else if constexpr (sizeof(T) == 2) {
-        xent_kernel<T, 1024, 16><<<grid_of(a.rows), 1024, 0, s>>>(a);
+        return st != FO_OK ? st : bwd<T, true>(b, a.logp, s);
     }
+    if (a.vocab <= 1024) launch_xent<T, 64, 2>(a, s);
+    else if (a.vocab <= 8192) launch_xent<T, 256, 4>(a, s);
+    else if (a.vocab <= 32768) launch_xent<T, 1024, 4>(a, s);
+    else launch_xent<T, 1024, 8>(a, s);
     FO_LAUNCHED();
     return FO_OK;
 }
@@ -308,8 +334,7 @@ fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
 }  // namespace
 
 int64_t logp_workspace(int64_t rows, int32_t vocab) {
-    // the type is not known here: cross-entropy's copy of logp and lse where either type needs it
-    return part_bytes(rows, vocab) + (held(rows, vocab, 4) ? 0 : cdiv(rows * 8, 16) * 16);
+    return part_bytes(rows, vocab) + (held(rows, vocab) ? 0 : cdiv(rows * 8, 16) * 16);  // and fo_xent's logp and lse
 }
 
 fo_status launch_logp_fwd(int32_t dtype, const LogpArgs& a, void* ws, hipStream_t s) {
@@ -317,7 +342,7 @@ fo_status launch_logp_fwd(int32_t dtype, const LogpArgs& a, void* ws, hipStream_
 }
 
 fo_status launch_logp_bwd(int32_t dtype, const LogpArgs& a, hipStream_t s) {
-    return dtype == FO_DT_BF16 ? bwd<bf16_t>(a, s) : bwd<float>(a, s);
+    return dtype == FO_DT_BF16 ? bwd<bf16_t, false>(a, nullptr, s) : bwd<float, false>(a, nullptr, s);
 }
 
 fo_status launch_xent(int32_t dtype, const LogpArgs& a, void* ws, hipStream_t s) {

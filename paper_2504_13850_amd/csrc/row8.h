@@ -33,6 +33,13 @@ struct Eight {
         __builtin_memcpy(v, u, sizeof(u));
         return to_f(v[e]);
     }
+    __device__ __forceinline__ void put(int place, T x) {
+        T v[8];
+        __builtin_memcpy(v, u, sizeof(u));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e == place ? x : v[e];
+        __builtin_memcpy(u, v, sizeof(u));
+    }
     __device__ __forceinline__ static void store(T* p, const float* x, int n, bool vec) {
         u32x4 w[sizeof(T) / 2];
         if constexpr (sizeof(T) == 2)
