@@ -17,18 +17,32 @@ constexpr float kLeast = -3.402823466e38f;
 
 // Maximum and sum of exp(scale (raw - maximum)) over some terms by their raw logits.  The maximum starts from the least
 // finite number and not from -infinity, so that no difference of infinities arises: a sum of 0 has no terms, or none
-// but -infinity.  A NaN goes by the maximum and into the sum.  c = scale log2(e).
+// but -infinity.  A NaN goes by the maximum and into the sum.
 struct Part {
     float m, s;
 };
 constexpr Part kNone = {kLeast, 0.f};
+// scale log2(e) in two parts: with the first alone every term of a row is off the same way, log sum exp by some 1e-7,
+// and a loss over whole answers adds that up.  Cross-entropy, whose rows nothing adds up before they are rounded, does
+// with the first (167 us, 177 with both).
+struct Factor {
+    float hi, lo;
+};
+__device__ __forceinline__ Factor factor(float scale) {
+    const double c = (double)scale * 1.4426950408889634;
+    return {(float)c, (float)(c - (double)(float)c)};
+}
+__device__ __forceinline__ float term(float raw, float m, Factor c) {
+    const float x = raw - m;
+    return __builtin_amdgcn_exp2f(fmaf(x, c.hi, fmaxf(x, -1e4f) * c.lo));
+}
 __device__ __forceinline__ float term(float raw, float m, float c) { return __builtin_amdgcn_exp2f((raw - m) * c); }
-__device__ __forceinline__ Part join(Part a, Part b, float c) {
+__device__ __forceinline__ Part join(Part a, Part b, Factor c) {
     const float m = fmaxf(a.m, b.m);
     return {m, a.s * term(a.m, m, c) + b.s * term(b.m, m, c)};
 }
 template <int TPR>
-__device__ __forceinline__ Part team_join(Part p, float c, Part* lds) {
+__device__ __forceinline__ Part team_join(Part p, Factor c, Part* lds) {
 #pragma unroll
     for (int m = 1; m < (TPR < 64 ? TPR : 64); m *= 2)
         p = join(p, Part{__shfl_xor(p.m, m), __shfl_xor(p.s, m)}, c);
@@ -48,7 +62,7 @@ struct Row {
     float m, inv, rest;
     bool none;  // every term is 0
 };
-__device__ __forceinline__ Row row_of(Part p, float zt, float c) {
+__device__ __forceinline__ Row row_of(Part p, float zt, Factor c) {
     Row r;
     r.m = fmaxf(p.m, zt);
     const float others = p.s * term(p.m, r.m, c), all = others + term(zt, r.m, c);
@@ -59,7 +73,8 @@ __device__ __forceinline__ Row row_of(Part p, float zt, float c) {
 }
 // logp and lse, in 64 bits: a loss over whole answers adds up what they are off by.
 __device__ __forceinline__ float2 logs_of(Part p, float zt, float scale) {
-    const float c = scale * kLog2e, m = fmaxf(p.m, zt);
+    const Factor c = factor(scale);
+    const float m = fmaxf(p.m, zt);
     const double others = (double)p.s * term(p.m, m, c), all = others + term(zt, m, c);
     if (all == 0.0) return make_float2(-INFINITY, -INFINITY);
     const double away = ((double)zt - m) * scale;
@@ -83,7 +98,7 @@ __device__ __forceinline__ Eight<T, false> last_chunk(const T* row, int vocab) {
     return x;
 }
 template <class T>
-__device__ __forceinline__ void add_chunk(const Eight<T, false>& x, float c, Part& p) {
+__device__ __forceinline__ void add_chunk(const Eight<T, false>& x, Factor c, Part& p) {
     float m = p.m;
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = fmaxf(m, x.at(e));
@@ -105,7 +120,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) logp_fwd_kernel(LogpArg
     if (row >= a.rows) return;
     const int target = a.targets[row];
     const bool there = target >= 0 && target < a.vocab;
-    const float c2 = a.scale * kLog2e;
+    const Factor c2 = factor(a.scale);
     Part p = kNone;
     if (there) {
         const T* x = (const T*)a.logits + row * a.ld;
@@ -154,7 +169,7 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
     const int target = a.targets[row];
     float2 r = make_float2(0.f, 0.f);
     if (target >= 0 && target < a.vocab) {
-        const float c = a.scale * kLog2e;
+        const Factor c = factor(a.scale);
         Part p = kNone;
         for (int k = threadIdx.x; k < slices; k += 64) p = join(p, part[row * slices + k], c);
         p = team_join<64>(p, c, nullptr);
@@ -219,7 +234,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 
     }
     const T* x = (const T*)a.logits + row * a.ld;
     const float zt = to_f(x[target]);
-    const float c2 = a.scale * kLog2e;
+    const Factor c2 = factor(a.scale);
     const int chunks = a.vocab / 8;  // one at least
     Eight<T, false> u[NC];
 #pragma unroll
@@ -238,7 +253,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p.s += term(u[c].at(e), p.m, c2);
+        for (int e = 0; e < 8; ++e) p.s += term(u[c].at(e), p.m, c2.hi);
     p.s = team<TPR>(p.s, lds + 16, Add());  // every thread has read its logits: dlogits may lie over them
     const Row r = row_of(p, zt, c2);
     const float g = r.none ? 0.f : a.weight[row] * a.scale, k = r.none ? 0.f : g * r.inv;
@@ -248,7 +263,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 
         const int c0 = (t + c * TPR) * 8, n = min(8, a.vocab - c0);
         float d[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = k * term(u[c].at(e), r.m, c2);
+        for (int e = 0; e < 8; ++e) d[e] = k * term(u[c].at(e), r.m, c2.hi);
         if (target >> 3 == t + c * TPR)
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = e == (target & 7) ? -g * r.rest : d[e];
