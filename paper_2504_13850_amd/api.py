@@ -741,31 +741,60 @@ def fo_dropout_bwd(dy, dx, p: float, seed: int, offset: int, dbias=None, workspa
 
 
 # ------------------------------------------------------------------ a language model's step around its attention
-def _row_list(what, n, dt, dev, *tensors):
-    """The given tensors (None apart) are contiguous lists of n numbers of type dt on device dev."""
-    for t in tensors:
-        if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous() or t.get_device() != dev):
-            raise FoError(FO_EINVAL, f"{what}: contiguous {dt} tensors of {n} numbers on the operands' device")
+# These calls are short beside what Python adds to them: each tensor is asked once for what is checked and passed on.
+def _mat(what, t, ty, dev: int, rows: int, cols: int):
+    """Address and row stride of a [rows, cols] matrix of type ty on device dev."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise FoError(FO_EINVAL, f"{what}: a matrix of shape {tuple(shape)}, not {(rows, cols)}")
+    if t.dtype != ty or t.get_device() != dev or (strides[1] != 1 and cols > 1):
+        raise FoError(FO_EINVAL, f"{what}: operands of one type on one device with a contiguous last dimension")
+    return t.data_ptr(), strides[0] if rows > 1 else cols
 
 
-def _matrices(what, shape, *tensors):
-    """The given tensors (None apart) are matrices of one shape, with distinct rows."""
-    for t in tensors:
-        if t is not None and (t.dim() != 2 or t.shape != shape):
-            raise FoError(FO_EINVAL, f"{what}: matrices of shape {tuple(shape)}, not {tuple(t.shape)}")
+def _mat_or_none(what, t, ty, dev: int, rows: int, cols: int):
+    return (None, 0) if t is None else _mat(what, t, ty, dev, rows, cols)
 
 
-def _lds(t) -> int:
-    return 0 if t is None else _ld(t)
+def _list(what, t, ty, dev: int, n: int):
+    """Address of a contiguous tensor of n numbers of type ty on device dev (None apart)."""
+    if t is None:
+        return None
+    if t.dtype != ty or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise FoError(FO_EINVAL, f"{what}: contiguous {ty} tensors of {n} numbers on the operands' device")
+    return t.data_ptr()
 
 
-def _eight_bits(what, dev, *tensors):
-    """The given tensors are e4m3 matrices (or their bytes) on device dev with a contiguous last dimension."""
-    import torch
-    for t in tensors:
-        if (t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.dim() != 2 or t.get_device() != dev
-                or (t.stride(-1) != 1 and t.shape[-1] > 1)):
-            raise FoError(FO_EINVAL, f"{what}: 8-bit rows are float8_e4m3fn or uint8 matrices with a contiguous last dimension")
+def _scratch(what, ws, dev: int):
+    """Address and bytes of a workspace on device dev (None apart)."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev:
+        raise FoError(FO_EINVAL, f"{what}: an operand, result or workspace on another device than the others")
+    return ws.data_ptr(), _bytes(ws)
+
+
+def _shape2(what, t):
+    """Rows, columns, type and device of the matrix that a call's other tensors go by."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise FoError(FO_EINVAL, f"{what}: a matrix, not a tensor of shape {tuple(shape)}")
+    return shape[0], shape[1], t.dtype, t.get_device()
+
+
+_f8_types = None
+
+
+def _bytes8(what, t, dev: int, rows: int, cols: int):
+    """Address and row stride of a matrix of 8-bit rows: e4m3 elements or their bytes."""
+    global _f8_types
+    if _f8_types is None:
+        import torch
+        _f8_types = torch.float8_e4m3fn, torch.uint8
+    ty = t.dtype
+    if ty not in _f8_types:
+        raise FoError(FO_EINVAL, f"{what}: 8-bit rows are float8_e4m3fn or uint8 matrices, not {ty}")
+    return _mat(what, t, ty, dev, rows, cols)
 
 
 def _workspace(n) -> int:
@@ -776,153 +805,147 @@ def _workspace(n) -> int:
 
 def fo_embed_fwd(tokens, table, out, scale: float = 1.0, stream=None):
     """out[r] = scale table[tokens[r]], zeros where the token (int32) is outside the table."""
-    _same("fo_embed_fwd", table, table, out)
-    dev, rows = table.get_device(), tokens.numel()
-    _row_list("fo_embed_fwd", rows, _torch_types()[1], dev, tokens)
-    _matrices("fo_embed_fwd", (table.shape[0], table.shape[-1]), table)
-    _matrices("fo_embed_fwd", (rows, table.shape[1]), out)
-    _on_gpu("fo_embed_fwd", dev, stream)
-    _check(lib().fo_embed_fwd(_dtype(table), rows, table.shape[1], table.shape[0], tokens.data_ptr(), table.data_ptr(),
-                              _ld(table), scale, out.data_ptr(), _ld(out), _stream(stream)))
+    what = "fo_embed_fwd"
+    vocab, cols, ty, dev = _shape2(what, table)
+    rows = tokens.numel()
+    dt, tok = _dtype(table), _list(what, tokens, _torch_types()[1], dev, rows)
+    table_at, out_at = _mat(what, table, ty, dev, vocab, cols), _mat(what, out, ty, dev, rows, cols)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_embed_fwd(dt, rows, cols, vocab, tok, *table_at, scale, *out_at, _stream(stream)))
 
 
 def fo_embed_workspace(rows: int, cols: int, vocab: int) -> int:
-    return _workspace(lib().fo_embed_workspace(rows, cols, vocab))
+    return _workspace((_lib or lib()).fo_embed_workspace(rows, cols, vocab))
 
 
 def fo_embed_bwd(tokens, dout, dtable, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None):
     """dtable[v] = scale times the sum of dout's rows of token v (added to what it holds if accumulate)."""
-    _same("fo_embed_bwd", dtable, dtable, dout)
-    dev, rows = dtable.get_device(), tokens.numel()
-    _row_list("fo_embed_bwd", rows, _torch_types()[1], dev, tokens)
-    _matrices("fo_embed_bwd", (dtable.shape[0], dtable.shape[-1]), dtable)
-    _matrices("fo_embed_bwd", (rows, dtable.shape[1]), dout)
-    _on_gpu("fo_embed_bwd", dev, stream, workspace)
-    _check(lib().fo_embed_bwd(_dtype(dtable), rows, dtable.shape[1], dtable.shape[0], tokens.data_ptr(),
-                              dout.data_ptr(), _ld(dout), scale, 1 if accumulate else 0, dtable.data_ptr(),
-                              _ld(dtable), _dptr(workspace), _bytes(workspace), _stream(stream)))
+    what = "fo_embed_bwd"
+    vocab, cols, ty, dev = _shape2(what, dtable)
+    rows = tokens.numel()
+    dt, tok = _dtype(dtable), _list(what, tokens, _torch_types()[1], dev, rows)
+    dtable_at, dout_at = _mat(what, dtable, ty, dev, vocab, cols), _mat(what, dout, ty, dev, rows, cols)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_embed_bwd(dt, rows, cols, vocab, tok, *dout_at, scale, 1 if accumulate else 0, *dtable_at,
+                                        *_scratch(what, workspace, dev), _stream(stream)))
+
+
+def _norm_operands(what, x, w, residual, h):
+    rows, cols, ty, dev = _shape2(what, x)
+    return (rows, cols, ty, dev, _dtype(x), _mat(what, x, ty, dev, rows, cols),
+            _mat_or_none(what, residual, ty, dev, rows, cols), _list(what, w, ty, dev, cols),
+            _mat_or_none(what, h, ty, dev, rows, cols))
 
 
 def fo_rmsnorm_fwd(x, w, y, rstd, eps: float, residual=None, h=None, stream=None):
     """h = x + residual, rstd = 1 / sqrt(mean h^2 + eps), y = h rstd w; residual, h, w and rstd may be None."""
-    _same("fo_rmsnorm_fwd", x, x, y, residual, h, w)
-    _matrices("fo_rmsnorm_fwd", x.shape, x, y, residual, h)
-    (rows, cols), dev = x.shape, x.get_device()
-    _row_list("fo_rmsnorm_fwd", cols, x.dtype, dev, w)
-    _row_list("fo_rmsnorm_fwd", rows, _torch_types()[2], dev, rstd)
-    _on_gpu("fo_rmsnorm_fwd", dev, stream)
-    _check(lib().fo_rmsnorm_fwd(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _addr(residual), _lds(residual), _addr(w),
-                                eps, _addr(h), _lds(h), y.data_ptr(), _ld(y), _addr(rstd), _stream(stream)))
+    what = "fo_rmsnorm_fwd"
+    rows, cols, ty, dev, dt, x_at, res_at, w_at, h_at = _norm_operands(what, x, w, residual, h)
+    y_at, r_at = _mat(what, y, ty, dev, rows, cols), _list(what, rstd, _torch_types()[2], dev, rows)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_rmsnorm_fwd(dt, rows, cols, *x_at, *res_at, w_at, eps, *h_at, *y_at, r_at, _stream(stream)))
 
 
 def fo_rmsnorm_workspace(rows: int, cols: int) -> int:
-    return _workspace(lib().fo_rmsnorm_workspace(rows, cols))
+    return _workspace((_lib or lib()).fo_rmsnorm_workspace(rows, cols))
 
 
 def fo_rmsnorm_bwd(dy, h, w, rstd, dx, dw=None, dres=None, workspace=None, stream=None):
     """The gradients of x (and residual) and of w; h and rstd as the forward call left them (h = x without a residual)."""
-    _same("fo_rmsnorm_bwd", dy, dy, h, w, dx, dw, dres)
-    _matrices("fo_rmsnorm_bwd", dy.shape, dy, h, dx, dres)
-    (rows, cols), dev = dy.shape, dy.get_device()
-    _row_list("fo_rmsnorm_bwd", cols, dy.dtype, dev, w, dw)
-    _row_list("fo_rmsnorm_bwd", rows, _torch_types()[2], dev, rstd)
-    _on_gpu("fo_rmsnorm_bwd", dev, stream, workspace)
-    _check(lib().fo_rmsnorm_bwd(_dtype(dy), rows, cols, dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h), _addr(w),
-                                rstd.data_ptr(), _addr(dres), _lds(dres), dx.data_ptr(), _ld(dx), _addr(dw),
-                                _addr(workspace), _bytes(workspace), _stream(stream)))
+    what = "fo_rmsnorm_bwd"
+    rows, cols, ty, dev, dt, dy_at, dres_at, w_at, h_at = _norm_operands(what, dy, w, dres, h)
+    if h is None or rstd is None:
+        raise FoError(FO_EINVAL, "fo_rmsnorm_bwd: h and rstd as the forward call left them")
+    dx_at, dw_at = _mat(what, dx, ty, dev, rows, cols), _list(what, dw, ty, dev, cols)
+    r_at = _list(what, rstd, _torch_types()[2], dev, rows)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_rmsnorm_bwd(dt, rows, cols, *dy_at, *h_at, w_at, r_at, *dres_at, *dx_at, dw_at,
+                                          *_scratch(what, workspace, dev), _stream(stream)))
 
 
 def fo_rmsnorm_f8(x, w, y8, y_scale, eps: float, residual=None, h=None, stream=None):
     """fo_rmsnorm_fwd with y as e4m3 rows and an fp32 scale for each."""
-    _same("fo_rmsnorm_f8", x, x, residual, h, w)
-    _matrices("fo_rmsnorm_f8", x.shape, x, y8, residual, h)
-    (rows, cols), dev = x.shape, x.get_device()
-    _eight_bits("fo_rmsnorm_f8", dev, y8)
-    _row_list("fo_rmsnorm_f8", cols, x.dtype, dev, w)
-    _row_list("fo_rmsnorm_f8", rows, _torch_types()[2], dev, y_scale)
-    _on_gpu("fo_rmsnorm_f8", dev, stream)
-    _check(lib().fo_rmsnorm_f8(_dtype(x), rows, cols, x.data_ptr(), _ld(x), _addr(residual), _lds(residual), _addr(w),
-                               eps, _addr(h), _lds(h), y8.data_ptr(), _ld(y8), y_scale.data_ptr(), _stream(stream)))
+    what = "fo_rmsnorm_f8"
+    rows, cols, ty, dev, dt, x_at, res_at, w_at, h_at = _norm_operands(what, x, w, residual, h)
+    y_at, s_at = _bytes8(what, y8, dev, rows, cols), _list(what, y_scale, _torch_types()[2], dev, rows)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_rmsnorm_f8(dt, rows, cols, *x_at, *res_at, w_at, eps, *h_at, *y_at, s_at, _stream(stream)))
 
 
 def fo_quant_f8(x, y8, y_scale, stream=None):
     """The rows of x as e4m3 with an fp32 scale for each."""
-    _same("fo_quant_f8", x, x)
-    _matrices("fo_quant_f8", x.shape, x, y8)
-    dev = x.get_device()
-    _eight_bits("fo_quant_f8", dev, y8)
-    _row_list("fo_quant_f8", x.shape[0], _torch_types()[2], dev, y_scale)
-    _on_gpu("fo_quant_f8", dev, stream)
-    _check(lib().fo_quant_f8(_dtype(x), x.shape[0], x.shape[1], x.data_ptr(), _ld(x), y8.data_ptr(), _ld(y8),
-                             y_scale.data_ptr(), _stream(stream)))
+    what = "fo_quant_f8"
+    rows, cols, ty, dev = _shape2(what, x)
+    dt, x_at, y_at = _dtype(x), _mat(what, x, ty, dev, rows, cols), _bytes8(what, y8, dev, rows, cols)
+    s_at = _list(what, y_scale, _torch_types()[2], dev, rows)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_quant_f8(dt, rows, cols, *x_at, *y_at, s_at, _stream(stream)))
 
 
 def fo_gemm_f8_workspace(M: int, N: int, K: int) -> int:
-    return _workspace(lib().fo_gemm_f8_workspace(M, N, K))
+    return _workspace((_lib or lib()).fo_gemm_f8_workspace(M, N, K))
 
 
 def fo_gemm_f8(a, a_scale, b, b_scale, c, workspace=None, stream=None):
     """c [M, N] = a [M, K] b [N, K]^T of 8-bit rows times their scales (None: ones)."""
-    _same("fo_gemm_f8", c, c)
-    dev = c.get_device()
-    _eight_bits("fo_gemm_f8", dev, a, b)
-    (M, K), N = a.shape, b.shape[0]
-    _matrices("fo_gemm_f8", (N, K), b)
-    _matrices("fo_gemm_f8", (M, N), c)
-    f32 = _torch_types()[2]
-    _row_list("fo_gemm_f8", M, f32, dev, a_scale)
-    _row_list("fo_gemm_f8", N, f32, dev, b_scale)
-    _on_gpu("fo_gemm_f8", dev, stream, workspace)
-    _check(lib().fo_gemm_f8(_dtype(c), M, N, K, a.data_ptr(), _ld(a), _addr(a_scale), b.data_ptr(), _ld(b),
-                            _addr(b_scale), c.data_ptr(), _ld(c), _addr(workspace), _bytes(workspace), _stream(stream)))
+    what = "fo_gemm_f8"
+    M, N, ty, dev = _shape2(what, c)
+    K, f32 = a.shape[-1], _torch_types()[2]
+    dt, c_at = _dtype(c), _mat(what, c, ty, dev, M, N)
+    a_at, b_at = _bytes8(what, a, dev, M, K), _bytes8(what, b, dev, N, K)
+    sa, sb = _list(what, a_scale, f32, dev, M), _list(what, b_scale, f32, dev, N)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_gemm_f8(dt, M, N, K, *a_at, sa, *b_at, sb, *c_at, *_scratch(what, workspace, dev),
+                                      _stream(stream)))
 
 
 def fo_logp_workspace(rows: int, vocab: int) -> int:
     """Bytes of workspace for fo_logp_fwd and fo_xent."""
-    return _workspace(lib().fo_logp_workspace(rows, vocab))
+    return _workspace((_lib or lib()).fo_logp_workspace(rows, vocab))
 
 
-def _logits(what, logits, targets, dlogits, stream, workspace, *lists):
-    _same(what, logits, logits, dlogits)
-    _matrices(what, logits.shape, logits, dlogits)
-    rows, dev = logits.shape[0], logits.get_device()
-    _row_list(what, rows, _torch_types()[1], dev, targets)
-    _row_list(what, rows, _torch_types()[2], dev, *lists)
-    _on_gpu(what, dev, stream, workspace)
-    return _dtype(logits), rows, logits.shape[1], logits.data_ptr(), _ld(logits), targets.data_ptr()
+def _logits(what, logits, targets, stream):
+    rows, vocab, ty, dev = _shape2(what, logits)
+    _on_gpu(what, dev, stream)
+    head = (_dtype(logits), rows, vocab, *_mat(what, logits, ty, dev, rows, vocab),
+            _list(what, targets, _torch_types()[1], dev, rows))
+    return head, rows, vocab, ty, dev, _torch_types()[2]
 
 
 def fo_logp_fwd(logits, targets, logp, lse=None, scale: float = 1.0, workspace=None, stream=None):
     """logp[r] = z_t - log sum exp z of z = scale logits[r], t = targets[r] (0 where t is outside the vocabulary)."""
-    head = _logits("fo_logp_fwd", logits, targets, None, stream, workspace, logp, lse)
-    _check(lib().fo_logp_fwd(*head, scale, logp.data_ptr(), _addr(lse), _addr(workspace), _bytes(workspace),
-                             _stream(stream)))
+    what = "fo_logp_fwd"
+    head, rows, _, _, dev, f32 = _logits(what, logits, targets, stream)
+    _check((_lib or lib()).fo_logp_fwd(*head, scale, _list(what, logp, f32, dev, rows), _list(what, lse, f32, dev, rows),
+                                       *_scratch(what, workspace, dev), _stream(stream)))
 
 
 def fo_logp_bwd(logits, targets, logp, lse, dlogp, dlogits, scale: float = 1.0, stream=None):
     """The gradient of the logits from that of logp; logp and lse as the forward call left them."""
-    head = _logits("fo_logp_bwd", logits, targets, dlogits, stream, None, logp, lse, dlogp)
-    _check(lib().fo_logp_bwd(*head, scale, logp.data_ptr(), lse.data_ptr(), dlogp.data_ptr(), dlogits.data_ptr(),
-                             _ld(dlogits), _stream(stream)))
+    what = "fo_logp_bwd"
+    head, rows, vocab, ty, dev, f32 = _logits(what, logits, targets, stream)
+    lists = [_list(what, t, f32, dev, rows) for t in (logp, lse, dlogp)]
+    _check((_lib or lib()).fo_logp_bwd(*head, scale, *lists, *_mat(what, dlogits, ty, dev, rows, vocab), _stream(stream)))
 
 
 def fo_xent(logits, targets, weight, loss, dlogits, scale: float = 1.0, workspace=None, stream=None):
     """loss[r] = -logp[r], and dlogits the gradient of sum weight[r] loss[r]."""
-    head = _logits("fo_xent", logits, targets, dlogits, stream, workspace, weight, loss)
-    _check(lib().fo_xent(*head, scale, weight.data_ptr(), loss.data_ptr(), dlogits.data_ptr(), _ld(dlogits),
-                         _addr(workspace), _bytes(workspace), _stream(stream)))
+    what = "fo_xent"
+    head, rows, vocab, ty, dev, f32 = _logits(what, logits, targets, stream)
+    _check((_lib or lib()).fo_xent(*head, scale, _list(what, weight, f32, dev, rows), _list(what, loss, f32, dev, rows),
+                                   *_mat(what, dlogits, ty, dev, rows, vocab), *_scratch(what, workspace, dev),
+                                   _stream(stream)))
 
 
 def fo_pref_loss(logp, ref, begin, end, loss, reward, dlogp=None, beta: float = 0.1, smooth: float = 0.0,
                  mean: bool = False, dloss: float = 1.0, stream=None):
     """The preference loss of answers in pairs, rows [begin[q], end[q]) of logp and ref: loss[pair], reward[answer],
     and dlogp, the gradient of dloss sum loss (rows of no answer are left as they are)."""
-    f32, dev, pairs = _torch_types()[2], logp.get_device(), loss.numel()
-    _row_list("fo_pref_loss", logp.numel(), f32, dev, logp, ref, dlogp)
-    _row_list("fo_pref_loss", 2 * pairs, _torch_types()[1], dev, begin, end)
-    _row_list("fo_pref_loss", pairs, f32, dev, loss)
-    _row_list("fo_pref_loss", 2 * pairs, f32, dev, reward)
-    _on_gpu("fo_pref_loss", dev, stream)
-    _check(lib().fo_pref_loss(pairs, logp.numel(), begin.data_ptr(), end.data_ptr(), logp.data_ptr(), _addr(ref), beta,
-                              smooth, 1 if mean else 0, dloss, loss.data_ptr(), reward.data_ptr(), _addr(dlogp),
-                              _stream(stream)))
+    what = "fo_pref_loss"
+    (_, i32, f32), rows, pairs, dev = _torch_types(), logp.numel(), loss.numel(), logp.get_device()
+    logp_at, ref_at, d_at = (_list(what, t, f32, dev, rows) for t in (logp, ref, dlogp))
+    begin_at, end_at = _list(what, begin, i32, dev, 2 * pairs), _list(what, end, i32, dev, 2 * pairs)
+    loss_at, reward_at = _list(what, loss, f32, dev, pairs), _list(what, reward, f32, dev, 2 * pairs)
+    _on_gpu(what, dev, stream)
+    _check((_lib or lib()).fo_pref_loss(pairs, rows, begin_at, end_at, logp_at, ref_at, beta, smooth, 1 if mean else 0,
+                                        dloss, loss_at, reward_at, d_at, _stream(stream)))
