@@ -183,7 +183,8 @@ FO_API fo_status fo_embed_bwd(int32_t dtype, int64_t rows, int32_t cols, int32_t
  * h (may be NULL) and rstd (fp32 [rows], may be NULL) are what the backward pass
  * needs; h is x itself without a residual.  y is computed from h before h is
  * rounded.  y or h may be x or residual, with its row stride; y is not h.
- * eps >= 0.  A row of zeros has y = 0, with eps = 0 too.
+ * eps >= 0.  A row of zeros has y = 0, with eps = 0 too.  Squares are summed in fp32:
+ * |h| has to stay below 1e19 over the root of cols, and above 1e-19 where eps = 0.
  * Errors: FO_EINVAL, FO_EHIP. */
 FO_API fo_status fo_rmsnorm_fwd(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t x_ld,
                                 const void* residual, int64_t res_ld, const void* w, float eps, void* h, int64_t h_ld,
@@ -222,8 +223,10 @@ FO_API fo_status fo_quant_f8(int32_t dtype, int64_t rows, int32_t cols, const vo
  * NULL (ones).  M >= 0; N, K >= 1.  In bf16 calls the products enter those sums by
  * eights, each cut below 2^-13 of the largest of its eight (the 8-bit matrix
  * instruction's way: some 1.4e-5 of the result's norm); fp32 calls keep all bits of
- * the products and take several times as long.  Rows that start 16-byte aligned
- * with K a multiple of 16 are read faster. */
+ * the products and take about twice as long.  Rows that start 16-byte aligned with
+ * K a multiple of 16 are read as they lie; with another K the workspace has room
+ * for copies that are; strides below 2^23 that are no multiple of 16 beside such a K
+ * cost most. */
 FO_API int64_t fo_gemm_f8_workspace(int64_t M, int32_t N, int32_t K);
 FO_API fo_status fo_gemm_f8(int32_t dtype, int64_t M, int32_t N, int32_t K, const uint8_t* a, int64_t lda,
                             const float* a_scale, const uint8_t* b, int64_t ldb, const float* b_scale, void* c,
@@ -232,7 +235,7 @@ FO_API fo_status fo_gemm_f8(int32_t dtype, int64_t M, int32_t N, int32_t K, cons
 /* ------------------------------------------------------------------ log probabilities
  * For row r of logits [rows][vocab] with target t = targets[r] (device int32):
  *
- *   z = scale logits_r                     scale > 0
+ *   z = scale logits_r                     scale > 0, scale log2(e) finite in fp32
  *   lse[r] = log sum_v exp(z_v)            natural logarithm
  *   logp[r] = z_t - lse[r]
  *

@@ -251,7 +251,7 @@ static fo_status check_logp(const char* what, int32_t dtype, int64_t rows, int32
     FO_TRY(check_sizes(what, dtype, rows, vocab));
     FO_TRY(check_rows(what, "logits", logits, ld, rows, vocab, elem_size(dtype), false));
     FO_TRY(check_vector(what, "targets", targets, rows, 4, false));
-    FO_CHECK(scale > 0.f && std::isfinite(scale), "%s: scale=%g", what, scale);
+    FO_CHECK(scale > 0.f && std::isfinite(scale * 1.4426950408889634f), "%s: scale=%g", what, scale);
     return FO_OK;
 }
 

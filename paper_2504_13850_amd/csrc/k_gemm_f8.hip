@@ -80,8 +80,8 @@ __device__ __forceinline__ void store4(const GemmF8Args& g, int64_t m, int n, co
 }
 
 // ------------------------------------------------------------------ any operands
-// Any strides, alignments and K: 64 rows by 64 columns a workgroup, 16 bytes at a time where a chunk lies inside the
-// row, byte by byte in its tail.
+// Small products of rows that no tile takes, and rows whose strides or starts alone are no multiple of 16: 64 rows by
+// 64 columns a workgroup, 16 bytes at a time where a chunk lies inside the row, byte by byte in its tail.
 template <class T>
 __global__ void __launch_bounds__(256) gemm_f8_any_kernel(GemmF8Args g) {
     constexpr int BK = 128, LD = BK + 16;
@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(64 * WM * WN) gemm_f8_tile_kernel(GemmF8Args g
 
 // ------------------------------------------------------------------ few rows of a
 // Up to 32 rows: b is read once, straight into registers; 16 columns a workgroup, whose waves take runs of k and join
-// their sums in order.  b's rows are the matrix instruction's first operand, a's 16 TM rows its second.
+// their sums in order.  b's rows are the matrix instruction's first operand, a's 16 TM rows its second.  Any strides,
+// alignments and K.
 template <class T, int TM, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) gemm_f8_few_kernel(GemmF8Args g) {
     constexpr int FLY = TM == 1 ? 8 : 4;  // steps of 128 in flight
@@ -319,12 +320,19 @@ __global__ void __launch_bounds__(64 * WAVES) gemm_f8_few_kernel(GemmF8Args g) {
     const uint8_t* a[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) a[i] = g.a + min((int64_t)(i * 16 + (lane & 15)), g.M - 1) * g.lda + (lane >> 4) * 32;
-    const auto load = [&](const uint8_t* p, int t) {  // chunks past K are zeros
-        const int k = t * 128 + (lane >> 4) * 32;
-        i32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-        if (k < g.K) lo = *(const i32x4*)(p + (int64_t)t * 128);
-        if (k + 16 < g.K) hi = *(const i32x4*)(p + (int64_t)t * 128 + 16);
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    const auto load = [&](const uint8_t* p, int t) {  // zeros past K
+        const int left = g.K - t * 128 - (lane >> 4) * 32;
+        i32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        p += (int64_t)t * 128;
+        if (left >= 32) {
+            __builtin_memcpy(&v, p, 32);
+        } else if (left > 0) {
+            uint8_t u[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) u[e] = e < left ? p[e] : 0;
+            __builtin_memcpy(&v, u, 32);
+        }
+        return v;
     };
     f32x4 acc[TM] = {};
     for (int t = first; t < last; t += FLY) {
@@ -403,6 +411,25 @@ int slices_of(int64_t M, int32_t N, int32_t K) {
     return tiles > kCUs / 4 || K < 8192 ? 1 : std::min(K / 2048, 16);
 }
 
+// Rows of K bytes to rows of `ld`, a multiple of 16 with zeros past K: chunks of a's rows, then of b's.
+__global__ void __launch_bounds__(256) gemm_f8_align_kernel(GemmF8Args g, uint8_t* __restrict__ a, uint8_t* __restrict__ b, int64_t ld) {
+    const int64_t chunks = ld / 16, id = (int64_t)block_of() * 256 + threadIdx.x, row = id / chunks, k = id % chunks * 16;
+    if (row >= g.M + g.N) return;
+    const bool first = row < g.M;
+    const uint8_t* from = first ? g.a + row * g.lda : g.b + (row - g.M) * g.ldb;
+    uint8_t v[16];
+    if (k + 16 <= g.K) {
+        __builtin_memcpy(v, from + k, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = k + e < g.K ? from[k + e] : 0;
+    }
+    __builtin_memcpy((first ? a + row * ld : b + (row - g.M) * ld) + k, v, 16);
+}
+// Whether a product whose rows have no multiple of 16 bytes is worth copies of its operands that have: with and without
+// them 100 x 1000 x 1001 takes 10 and 14 us, 2048 x 2048 x 2047 27 and 41, 8000 x 8000 x 8001 483 and 1756.
+bool copies_pay(int64_t M, int32_t N, int32_t K) { return K % 16 && M > 32 && (double)M * N * K >= 1e8; }
+
 template <class T, class Out, int BM, int BN, int WM, int WN, int STAGES>
 void launch_tiles(const GemmF8Args& g, int slices, hipStream_t s) {
     const int tm = (int)cdiv(g.M, BM), tn = (int)cdiv(g.N, BN), slice = (int)(cdiv(cdiv(g.K, 128), slices) * 128);
@@ -411,21 +438,10 @@ void launch_tiles(const GemmF8Args& g, int slices, hipStream_t s) {
 }
 
 template <class T>
-fo_status run(const GemmF8Args& g, float* part, hipStream_t s) {
-    const bool whole = g.K % 16 == 0 && g.lda < kTileStride && g.ldb < kTileStride && g.lda % 16 == 0 &&
-                       g.ldb % 16 == 0 && ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0;
+fo_status run_tiles(const GemmF8Args& g, float* part, hipStream_t s) {
     const auto tiles = [&](int side) { return cdiv(g.M, side) * cdiv(g.N, side); };
     const int slices = slices_of(g.M, g.N, g.K);
-    if (!whole) {
-        gemm_f8_any_kernel<T><<<grid_of(tiles(64)), 256, 0, s>>>(g);
-    } else if (few_rows(g)) {
-        const dim3 grid = grid_of(cdiv(g.N, 16));
-        // eight waves share k where columns are few (4 x 4096 x 4096: 6.5 us either way), else four (1 x 128000 x 4096:
-        // 88 us, 108 with eight)
-        if (g.M > 16) gemm_f8_few_kernel<T, 2, 8><<<grid, 512, 0, s>>>(g);
-        else if (g.N < 16 * 4 * kCUs) gemm_f8_few_kernel<T, 1, 8><<<grid, 512, 0, s>>>(g);
-        else gemm_f8_few_kernel<T, 1, 4><<<grid, 256, 0, s>>>(g);
-    } else if (slices > 1) {
+    if (slices > 1) {
         GemmF8Args h = g;
         h.c = part;
         h.ldc = g.N;
@@ -447,15 +463,52 @@ fo_status run(const GemmF8Args& g, float* part, hipStream_t s) {
     return FO_OK;
 }
 
-}  // namespace
-
-int64_t gemm_f8_workspace(int64_t M, int32_t N, int32_t K) {
-    const int slices = M ? slices_of(M, N, K) : 1;
+int64_t part_bytes(int64_t M, int32_t N, int32_t K) {
+    const int slices = slices_of(M, N, K);
     return slices > 1 ? cdiv((int64_t)slices * M * N * 4, 16) * 16 : 0;
 }
 
+template <class T>
+fo_status run(const GemmF8Args& g, char* ws, hipStream_t s) {
+    const bool whole = g.K % 16 == 0 && g.lda < kTileStride && g.ldb < kTileStride && g.lda % 16 == 0 &&
+                       g.ldb % 16 == 0 && ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0;
+    const int64_t ld = cdiv(g.K, 16) * 16;
+    if (few_rows(g)) {
+        const dim3 grid = grid_of(cdiv(g.N, 16));
+        // eight waves share k where columns are few (4 x 4096 x 4096: 6.5 us either way), else four (1 x 128000 x 4096:
+        // 88 us, 108 with eight)
+        if (g.M > 16) gemm_f8_few_kernel<T, 2, 8><<<grid, 512, 0, s>>>(g);
+        else if (g.N < 16 * 4 * kCUs) gemm_f8_few_kernel<T, 1, 8><<<grid, 512, 0, s>>>(g);
+        else gemm_f8_few_kernel<T, 1, 4><<<grid, 256, 0, s>>>(g);
+    } else if (whole) {
+        return run_tiles<T>(g, (float*)ws, s);
+    } else if (copies_pay(g.M, g.N, g.K) && ld < kTileStride) {
+        GemmF8Args h = g;
+        uint8_t *a = (uint8_t*)ws + part_bytes(g.M, g.N, (int32_t)ld), *b = a + g.M * ld;
+        gemm_f8_align_kernel<<<grid_of(cdiv((g.M + g.N) * (ld / 16), 256)), 256, 0, s>>>(g, a, b, ld);
+        FO_LAUNCHED();
+        h.a = a; h.b = b;
+        h.lda = h.ldb = ld;
+        h.K = (int32_t)ld;
+        return run_tiles<T>(h, (float*)ws, s);
+    } else {
+        gemm_f8_any_kernel<T><<<grid_of(cdiv(g.M, 64) * cdiv(g.N, 64)), 256, 0, s>>>(g);
+    }
+    FO_LAUNCHED();
+    return FO_OK;
+}
+
+}  // namespace
+
+int64_t gemm_f8_workspace(int64_t M, int32_t N, int32_t K) {
+    if (!M) return 0;
+    const int64_t ld = cdiv(K, 16) * 16;
+    if (!copies_pay(M, N, K)) return part_bytes(M, N, K);
+    return part_bytes(M, N, (int32_t)ld) + (M + N) * ld;
+}
+
 fo_status launch_gemm_f8(int32_t dtype, const GemmF8Args& g, void* ws, hipStream_t s) {
-    return dtype == FO_DT_BF16 ? run<bf16_t>(g, (float*)ws, s) : run<float>(g, (float*)ws, s);
+    return dtype == FO_DT_BF16 ? run<bf16_t>(g, (char*)ws, s) : run<float>(g, (char*)ws, s);
 }
 
 }  // namespace fo

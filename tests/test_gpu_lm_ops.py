@@ -251,6 +251,18 @@ def test_f8(dtype, rows, cols):
         assert q.untouched() and h.untouched()
 
 
+def test_f8_nan_keeps_to_its_row():
+    torch = torch_cuda()
+    announce("8-bit rows, NaN and infinity")
+    x = _normal(1, 4, 300)
+    x[1, 299], x[2, 0] = NAN, float("inf")
+    q, s = torch.empty(x.shape, dtype=torch.uint8, device="cuda"), torch.empty(4, device="cuda")
+    A.fo_quant_f8(x, q, s)
+    v = R.f8_values()[q.cpu().numpy()] * _np(s)[:, None]
+    assert np.isnan(v[1, 299]) and not np.isnan(v[1, :299]).any() and np.isnan(v[2]).any()
+    _check_f8(_np(x[[0, 3]]), q[[0, 3]].cpu().numpy(), _np(s[[0, 3]]), 4 * F)
+
+
 def test_f8_rounding():
     """Every e4m3 value comes back as itself, ties go to the even neighbour, and tiny rows keep within their range."""
     torch = torch_cuda()
@@ -278,7 +290,8 @@ def test_f8_rounding():
 GEMM = [(1, 1, 1), (1, 5, 16), (3, 64, 128), (7, 100, 77), (16, 16, 4096), (1, 4096, 512), (5, 130, 2064), (33, 257, 384),
         (64, 512, 1024), (65, 300, 100), (130, 129, 640), (257, 640, 256), (300, 1000, 1500), (520, 513, 2048),
         (1030, 768, 912), (2, 20, 9001),
-        (40, 100, 8208), (70, 130, 16400), (130, 64, 12304), (20, 17000, 160), (700, 4100, 272), (2049, 2600, 400), (3400, 3500, 160)]
+        (40, 100, 8208), (70, 130, 16400), (130, 64, 12304), (20, 17000, 160), (700, 4100, 272), (2049, 2600, 400), (3400, 3500, 160),
+        (100, 1000, 1001), (520, 513, 2047), (40, 100, 28209), (32, 70, 515)]
 
 
 def _bytes(seed, rows, cols):
@@ -299,7 +312,7 @@ def test_gemm_f8(dtype, M, N, K):
         announce(f"8-bit product {dtype} {M} x {N} x {K}, pad {pad}")
         a, b = _bytes(M + K, M, K), _bytes(N + 7, N, K)
         am, bm = (Mat(len(x), K, "f8", pad, shift, torch.from_numpy(x).cuda()) for x in (a, b))
-        sa, sb = (None, None) if pad == 3 else (_normal(1, M).abs() + 0.1, _normal(2, N))
+        sa, sb = (None, None) if pad == 16 else (_normal(1, M).abs() + 0.1, _normal(2, N))
         c = Mat(M, N, dtype, pad, shift)
         A.fo_gemm_f8(am.t, sa, bm.t, sb, c.t, workspace=_ws(A.fo_gemm_f8_workspace(M, N, K)))
         want, size = R.gemm(v[a], None if sa is None else _np(sa), v[b], None if sb is None else _np(sb))

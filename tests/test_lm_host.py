@@ -141,6 +141,7 @@ def test_refuses(name, bad):
     ("fo_rmsnorm_f8", dict(y=X)), ("fo_quant_f8", dict(y=X)), ("fo_rmsnorm_bwd", dict(dx=X, dx_ld=9)),
     ("fo_rmsnorm_bwd", dict(dx=X + 64, dx_ld=9)), ("fo_rmsnorm_bwd", dict(dx=X + 128, dx_ld=9)),
     ("fo_logp_bwd", dict(d=X, d_ld=9)), ("fo_xent", dict(d=X, d_ld=9)), ("fo_gemm_f8", dict(c=X)),
+    ("fo_logp_fwd", dict(scale=3e38)), ("fo_xent", dict(scale=0.0)), ("fo_gemm_f8", dict(n=8, rows=100, cols=1000, ldc=1000, K=1001, lda=1001, ldb=1001)),
     ("fo_gemm_f8", dict(rows=1 << 27, cols=1 << 20, ldc=1 << 20)),
     ("fo_gemm_f8", dict(c=X + 64)), ("fo_embed_fwd", dict(out=X)), ("fo_embed_bwd", dict(dtable=X)),
     ("fo_embed_bwd", dict(rows=(1 << 28) + 1)),
