@@ -126,8 +126,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) logp_fwd_kernel(LogpArg
     const bool there = target >= 0 && target < a.vocab;
     const Factor c2 = factor(a.scale);
     Part p = kNone;
+    float zt = 0.f;
     if (there) {
         const T* x = (const T*)a.logits + row * a.ld;
+        if (!SLICED) zt = to_f(x[target]);
         const int chunks = a.vocab / 8, each = SLICED ? (chunks + slices - 1) / slices : chunks;
         const int slice = SLICED ? (int)(id % slices) : 0, first = min(chunks, slice * each), last = min(chunks, first + each);
         int c = first + t;
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) logp_fwd_kernel(LogpArg
         return;
     }
     float2 r = make_float2(0.f, 0.f);
-    if (there) r = logs_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
+    if (there) r = logs_of(p, zt, a.scale);
     a.logp[row] = r.x;
     if (a.lse) a.lse[row] = r.y;
 }
@@ -174,10 +176,11 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
     float2 r = make_float2(0.f, 0.f);
     if (target >= 0 && target < a.vocab) {
         const Factor c = factor(a.scale);
+        const float zt = to_f(((const T*)a.logits)[row * a.ld + target]);
         Part p = kNone;
         for (int k = threadIdx.x; k < slices; k += 64) p = join(p, part[row * slices + k], c);
         p = team_join<64>(p, c, nullptr);
-        r = logs_of(p, to_f(((const T*)a.logits)[row * a.ld + target]), a.scale);
+        r = logs_of(p, zt, a.scale);
     }
     if (threadIdx.x) return;
     a.logp[row] = r.x;
@@ -275,11 +278,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 
     }
 }
 
-// Workgroups along a row so that few long rows fill the chip: about two workgroups a CU, 4096 logits each or more.
+// Workgroups along a row so that few long rows fill the chip: about two workgroups a CU, 4096 logits each or more.  Up
+// to 65536 logits one workgroup of 1024 threads a row is as fast in one launch (60 rows of 32000 bf16 8.0 us, 8.2 in
+// two; 5 rows of 128000 fp32 12.7 and 7.7).
 constexpr int64_t kWgs = 512;
+constexpr int32_t kOneWg = 65536;
 int slices_of(int64_t rows, int32_t vocab) {
-    if (rows >= kWgs || rows < 1) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(kWgs / rows, vocab / 4096));
+    if (rows >= kWgs || rows < 1 || vocab <= kOneWg) return 1;
+    return (int)std::min<int64_t>(kWgs / rows, vocab / 4096);
 }
 int64_t part_bytes(int64_t rows, int32_t vocab) {
     const int n = slices_of(rows, vocab);
@@ -295,8 +301,10 @@ fo_status fwd(const LogpArgs& a, void* ws, hipStream_t s) {
         logp_join_kernel<T><<<grid_of(a.rows), 64, 0, s>>>(a, (const Part*)ws, n);
     } else if (a.vocab <= 2048) {
         logp_fwd_kernel<T, 64, false><<<grid_of(cdiv(a.rows, 4)), 256, 0, s>>>(a, nullptr, 1);
-    } else {
+    } else if (a.vocab <= 8192 || a.rows >= kWgs) {
         logp_fwd_kernel<T, 256, false><<<grid_of(a.rows), 256, 0, s>>>(a, nullptr, 1);
+    } else {
+        logp_fwd_kernel<T, 1024, false><<<grid_of(a.rows), 1024, 0, s>>>(a, nullptr, 1);
     }
     FO_LAUNCHED();
     return FO_OK;
@@ -321,9 +329,9 @@ fo_status bwd(const LogpArgs& a, float* loss, hipStream_t s) {
     return FO_OK;
 }
 
-// Rows that a workgroup holds in registers: 8 NC logits a thread, a whole chunk at least.  Longer ones, and a few rows
-// that one workgroup each would be slow for, go through the forward pass and the gradient.
-bool held(int64_t rows, int32_t vocab) { return slices_of(rows, vocab) == 1 && vocab >= 8 && vocab <= 65536; }
+// Rows that a workgroup holds in registers: 8 NC logits a thread, a whole chunk at least.  Others go through the forward
+// pass and the gradient.
+bool held(int32_t vocab) { return vocab >= 8 && vocab <= kOneWg; }
 
 template <class T, int TPR, int NC>
 void launch_xent(const LogpArgs& a, hipStream_t s) {
@@ -335,7 +343,7 @@ void launch_xent(const LogpArgs& a, hipStream_t s) {
 
 template <class T>
 fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
-    if (!held(a.rows, a.vocab)) {
+    if (!held(a.vocab)) {
         LogpArgs b = a;
         b.logp = (float*)((char*)ws + part_bytes(a.rows, a.vocab));
         b.lse = b.logp + a.rows;
@@ -353,7 +361,7 @@ fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
 }  // namespace
 
 int64_t logp_workspace(int64_t rows, int32_t vocab) {
-    return part_bytes(rows, vocab) + (held(rows, vocab) ? 0 : cdiv(rows * 8, 16) * 16);  // and fo_xent's logp and lse
+    return part_bytes(rows, vocab) + (held(vocab) ? 0 : cdiv(rows * 8, 16) * 16);  // and fo_xent's logp and lse
 }
 
 fo_status launch_logp_fwd(int32_t dtype, const LogpArgs& a, void* ws, hipStream_t s) {

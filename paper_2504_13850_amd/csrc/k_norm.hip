@@ -209,16 +209,52 @@ int64_t bwd_parts(int64_t rows, int32_t cols) {
     return n <= 512 ? std::max<int64_t>(1, n) : std::min<int64_t>(1024, std::max<int64_t>(512, n / 2));
 }
 
-template <class T, class S, bool NT>
-__global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a) {
+// 64 columns of dw, all rows: eight threads along the columns, the others' sums joined in order.
+template <class T, int THREADS>
+__device__ void dw_columns(const NormBwdArgs& a, int64_t id, float* sums) {
+    constexpr int TEAMS = THREADS / 8;
+    const int tx = threadIdx.x % 8, ty = threadIdx.x / 8;
+    const int64_t c0 = id * 64 + tx * 8;
+    const int n = (int)min((int64_t)8, a.cols - c0);
+    float dw[8] = {};
+    if (n > 0) {
+#pragma unroll 4
+        for (int64_t row = ty; row < a.rows; row += TEAMS) {
+            Eight<T, false> g, x;
+            g.load((const T*)a.dy + row * a.dy_ld + c0, n, n == 8);
+            x.load((const T*)a.h + row * a.h_ld + c0, n, n == 8);
+            const float r = a.rstd[row];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dw[e] += g.at(e) * (x.at(e) * r);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[ty * 64 + tx * 8 + e] = dw[e];
+    __syncthreads();
+    const int64_t c = id * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= a.cols) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < TEAMS; ++k) s += sums[k * 64 + threadIdx.x];
+    ((T*)a.dw)[c] = from_f<T>(s);
+}
+
+// NT: operands past the caches, and dx.  FEW: workgroups past `rows_wgs` write dw, from dy and h read once more, in the
+// same launch; else each leaves its rows' part of it.
+template <class T, class S, bool NT, bool FEW>
+__global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a, int rows_wgs) {
     __shared__ float lds[2][16];
-    __shared__ float sums[S::RPW > 1 ? 8 * S::THREADS : 1];
+    __shared__ float sums[S::RPW > 1 || FEW ? 8 * S::THREADS : 1];
+    if (FEW && (int)blockIdx.x >= rows_wgs) {
+        dw_columns<T, S::THREADS>(a, (int)blockIdx.x - rows_wgs, sums);
+        return;
+    }
     const int t = threadIdx.x % S::TPR, ty = threadIdx.x / S::TPR;
     float w[S::NC][8], dw[S::NC][8] = {};
 #pragma unroll
     for (int c = 0; c < S::NC; ++c) load_w<T>(a.w, (t + c * S::TPR) * 8, min(8, a.cols - (t + c * S::TPR) * 8), w[c]);
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * S::RPW + ty; row < a.rows; row += (int64_t)gridDim.x * S::RPW) {
+    for (int64_t row = (int64_t)blockIdx.x * S::RPW + ty; row < a.rows; row += (int64_t)rows_wgs * S::RPW) {
         Eight<T, NT> dy[S::NC], h[S::NC], dr[S::NC];
         const float r = a.rstd[row];
         float dot = 0.f;
@@ -250,7 +286,7 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a) {
             if (n > 0) Eight<T, NT>::store((T*)a.dx + row * a.dx_ld + c0, dx, n, n == 8);
         }
     }
-    if (!a.part) return;
+    if (FEW || !a.part) return;
 #pragma unroll
     for (int c = 0; c < S::NC; ++c) {
         if constexpr (S::RPW > 1) {  // the teams' sums, in order
@@ -329,14 +365,25 @@ __global__ void __launch_bounds__(256) norm_dw_long_kernel(NormBwdArgs a, int pa
     for (int e = 0; e < n; ++e) a.part[blockIdx.y * (int64_t)a.cols + c0 + e] = dw[e];
 }
 
+// Up to 512 rows dw is cheaper read for than joined in a second launch (a pass forward and backward, bf16: 4 rows of 768
+// 7.6 us and 10.3, 512 of 8192 20 and 35; 1024 of 768 14 and 12), unless dx lies over what it reads.
+constexpr int64_t kFewRows = 512;
 template <class T>
-fo_status bwd(const NormBwdArgs& a, void* dw, hipStream_t s) {
+fo_status bwd(const NormBwdArgs& args, void* dw, hipStream_t s) {
+    NormBwdArgs a = args;
     const int parts = (int)bwd_parts(a.rows, a.cols);
+    const bool few = dw && a.rows <= kFewRows && a.rows > 0 && a.cols <= Shape<1024, 1024, 4>::COLS && a.dx != a.dy && a.dx != a.h;
     if (a.rows) {
         const bool held = with_shape(a.cols, [&](auto shape) {
             using S = decltype(shape);
-            if (past_caches<T>(a.rows, a.cols)) norm_bwd_kernel<T, S, true><<<parts, S::THREADS, 0, s>>>(a);
-            else norm_bwd_kernel<T, S, false><<<parts, S::THREADS, 0, s>>>(a);
+            if (few) {
+                a.dw = dw;
+                norm_bwd_kernel<T, S, false, true><<<parts + (int)cdiv(a.cols, 64), S::THREADS, 0, s>>>(a, parts);
+            } else if (past_caches<T>(a.rows, a.cols)) {
+                norm_bwd_kernel<T, S, true, false><<<parts, S::THREADS, 0, s>>>(a, parts);
+            } else {
+                norm_bwd_kernel<T, S, false, false><<<parts, S::THREADS, 0, s>>>(a, parts);
+            }
         });
         if (!held) {
             if (a.part) {
@@ -347,7 +394,7 @@ fo_status bwd(const NormBwdArgs& a, void* dw, hipStream_t s) {
         }
         FO_LAUNCHED();
     }
-    return dw ? column_sums<T>(a.part, a.rows ? parts : 0, a.cols, (T*)dw, s) : FO_OK;
+    return dw && !few ? column_sums<T>(a.part, a.rows ? parts : 0, a.cols, (T*)dw, s) : FO_OK;
 }
 
 }  // namespace

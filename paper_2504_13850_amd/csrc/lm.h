@@ -52,6 +52,7 @@ struct NormBwdArgs {
     void* dx;
     int64_t dx_ld;
     float* part;  // [parts][cols] sums of dw, or NULL
+    void* dw;     // where the rows are few: see norm_bwd_kernel
 };
 int64_t norm_workspace(int64_t rows, int32_t cols);
 fo_status launch_norm_bwd(int32_t dtype, const NormBwdArgs& a, void* dw, hipStream_t s);
