@@ -157,7 +157,7 @@ FO_API fo_status fo_dropout_bwd(int32_t dtype, int64_t rows, int32_t cols, const
 /* ------------------------------------------------------------------ embedding
  * out_r = scale table[tokens[r]] over rows of `cols` elements; a token outside
  * [0, vocab) (padding) has a row of zeros and takes part in no gradient.  tokens:
- * device int32[rows].  ld: row strides in elements, >= cols.  cols up to 2^23.  The product is
+ * device int32[rows].  ld: row strides in elements, >= cols.  cols up to 2^22.  The product is
  * rounded once.  Errors: FO_EINVAL, FO_EHIP. */
 FO_API fo_status fo_embed_fwd(int32_t dtype, int64_t rows, int32_t cols, int32_t vocab, const int32_t* tokens,
                               const void* table, int64_t table_ld, float scale, void* out, int64_t out_ld,

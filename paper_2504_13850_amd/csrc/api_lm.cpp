@@ -61,8 +61,8 @@ fo_status check_workspace(const char* what, const void* ws, int64_t bytes, int64
     } while (0)
 
 // ------------------------------------------------------------------ embedding
-// 256 columns a workgroup in a launch's third dimension; 4096 rows a tile of the sort.
-constexpr int32_t kMaxEmbedCols = 1 << 23;
+// 128 columns a workgroup in a launch's third dimension; 4096 rows a tile of the sort.
+constexpr int32_t kMaxEmbedCols = 1 << 22;
 constexpr int64_t kMaxEmbedRows = int64_t(1) << 28;
 
 static fo_status check_embed(const char* what, int32_t dtype, int64_t rows, int32_t cols, int32_t vocab,

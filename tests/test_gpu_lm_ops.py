@@ -78,14 +78,16 @@ LAYOUTS = [(0, 0), (3, 1)]
 
 # ------------------------------------------------------------------ embedding
 EMBED = [(1, 1, 1), (1, 7, 3), (5, 8, 2), (33, 130, 32), (1203, 128, 32), (300, 77, 5000), (4096, 64, 1), (4097, 20, 600),
-         (9000, 24, 40000), (20000, 40, 70), (70000, 8, 1200), (17000, 9, 2200000)]
+         (9000, 24, 40000), (20000, 40, 70), (70000, 8, 1200), (17000, 9, 2200000),
+         (1024, 300, 5), (1024, 129, 1), (1025, 64, 900), (700, 16, 100003), (2048, 136, 40), (2, 9, 200000),
+         (512, 130, 3), (500, 264, 1), (512, 40, 300), (513, 40, 300)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols,vocab", EMBED)
 def test_embed(dtype, rows, cols, vocab):
     torch = torch_cuda()
-    for pad, shift in LAYOUTS if rows * cols < 1 << 17 and vocab < 10000 else LAYOUTS[:1]:
+    for pad, shift in LAYOUTS if rows * cols < 1 << 18 and vocab < 10000 else LAYOUTS[:1]:
         announce(f"embed {dtype} {rows} rows of {cols}, vocab {vocab}, pad {pad}")
         rng = np.random.default_rng(rows + cols)
         # a few tokens many times, many tokens rarely, some outside the table

@@ -145,8 +145,8 @@ def test_refuses(name, bad):
     ("fo_gemm_f8", dict(rows=1 << 27, cols=1 << 20, ldc=1 << 20)),
     ("fo_gemm_f8", dict(c=X + 64)), ("fo_embed_fwd", dict(out=X)), ("fo_embed_bwd", dict(dtable=X)),
     ("fo_embed_bwd", dict(rows=(1 << 28) + 1)),
-    ("fo_embed_fwd", dict(cols=(1 << 23) + 1, table_ld=1 << 24, out_ld=1 << 24)),
-    ("fo_embed_bwd", dict(cols=(1 << 23) + 1, dout_ld=1 << 24, dtable_ld=1 << 24)), ("fo_rmsnorm_bwd", dict(n=8)), ("fo_rmsnorm_bwd", dict(ws=X + 4)),
+    ("fo_embed_fwd", dict(cols=(1 << 22) + 1, table_ld=1 << 23, out_ld=1 << 23)),
+    ("fo_embed_bwd", dict(cols=(1 << 22) + 1, dout_ld=1 << 23, dtable_ld=1 << 23)), ("fo_rmsnorm_bwd", dict(n=8)), ("fo_rmsnorm_bwd", dict(ws=X + 4)),
     ("fo_rmsnorm_fwd", dict(rows=MANY, x_ld=1 << 31)), ("fo_logp_bwd", dict(rows=MANY, d_ld=1 << 31)),
     ("fo_xent", dict(rows=4, cols=1 << 20, x_ld=1 << 20, d_ld=1 << 20, n=16))], ids=str)
 def test_refuses_together(name, bad):
@@ -168,7 +168,7 @@ def test_accepts_no_rows():
 
 
 @pytest.mark.parametrize("call", [lambda: A.fo_embed_workspace(-1, 8, 8), lambda: A.fo_embed_workspace(1 << 29, 8, 8),
-                                  lambda: A.fo_embed_workspace(4, 0, 8), lambda: A.fo_embed_workspace(4, (1 << 23) + 1, 8), lambda: A.fo_embed_workspace(4, 8, 0),
+                                  lambda: A.fo_embed_workspace(4, 0, 8), lambda: A.fo_embed_workspace(4, (1 << 22) + 1, 8), lambda: A.fo_embed_workspace(4, 8, 0),
                                   lambda: A.fo_rmsnorm_workspace(-1, 8), lambda: A.fo_rmsnorm_workspace(4, 0),
                                   lambda: A.fo_gemm_f8_workspace(-1, 4, 4), lambda: A.fo_gemm_f8_workspace(4, 0, 4),
                                   lambda: A.fo_gemm_f8_workspace(4, 4, 0), lambda: A.fo_logp_workspace(-1, 4),
