@@ -1,4 +1,9 @@
 // Products of 8-bit rows with a scale each: c_mn = a_scale[m] b_scale[n] sum_k a_mk b_nk.
+//
+// Large ones are bound by the matrix instructions: 8192^3 in 425 to 437 us, 2510 to 2590 TFLOP/s (the library's 2730;
+// the instructions alone, from registers, 4330), at a clock that the load takes down to 1.95 GHz: 2990 in the loop over
+// k, 40 us for the tiles' first copies and their rows' way out.  Few rows of a are bound by reading b: 1 x 128000 x
+// 4096 in 88 us, 6.0 TB/s.  Between them the latency of copies, steps and stores that follow each other.
 #include <algorithm>
 
 #include "lm.h"
@@ -134,7 +139,7 @@ __global__ void __launch_bounds__(256) gemm_f8_any_kernel(GemmF8Args g) {
 
 // ------------------------------------------------------------------ tiles
 // Rows that start 16-byte aligned, K a multiple of 16.  BM x BN of c a workgroup, WM x WN waves; 128 of k a step, in
-// two stages of LDS that the copies fill without registers (lane l of a wave writes 16 bytes at the instruction's
+// two to four stages of LDS that the copies fill without registers (lane l of a wave writes 16 bytes at the instruction's
 // base + 16 l, so an instruction fills eight rows of 128 bytes).  Chunk c of row r lies at c ^ r % 8 ^ r / 8 % 8: eight
 // neighbouring rows, and sixteen, read one chunk from distinct banks.
 // As the compiler's own instruction the copy would be waited for before every read of LDS that it might write; here the
@@ -395,13 +400,15 @@ __global__ void __launch_bounds__(256) gemm_f8_join_kernel(GemmF8Args g, const f
 //   20    128000 1024   47        24
 //   32    4096   4096   9.5       17.5
 //   256   4096   4096             10.9     20.6                 23.9      43.9
-//   1024  4096   4096             30       23.7                 27.1      47.2
-//   2603  2304   768              16.3     16.3                 12.2      17.2
-//   2048  4096   4096             56       44.8                 35.1      50.7
-//   4096  4096   4096             104      86                   65.7      60.1
-//   8192  8192   8192             858      629                  521       431
+//   600   4096   4096                      19.0                 23.8
+//   1024  4096   4096             30       23.1                 27.1      47.2
+//   2603  2304   768              16.3     14.3                 12.4      17.2
+//   2048  4096   4096             56       42.6                 35.4      50.7
+//   4096  4096   4096             104      82                   65.7      61.9
+//   8192  8192   8192             858      615                  521       427
 // Tiles of 64 hold four stages and of 128 three where a CU has a workgroup or two at a time: the copies then have the
-// memory's latency for themselves.  From two rounds of workgroups on, two stages and two workgroups a CU hide it better.
+// memory's latency for themselves, and a lone tile of 128 is shared by eight waves (600 x 4096 x 4096 21.3 us with
+// four).  From two rounds of workgroups on, two stages and two workgroups a CU hide it better.
 constexpr int kCUs = 256;
 bool few_rows(const GemmF8Args& g) { return g.M <= 16 || (g.M <= 32 && cdiv(g.N, 64) < kCUs); }
 // Slices of k, of 2048 or more, where 64 x 64 tiles are few and k is long: 100 x 1024 x 8192 14.2 -> 11.8 us, 40 x 512 x
@@ -453,7 +460,7 @@ fo_status run_tiles(const GemmF8Args& g, float* part, hipStream_t s) {
     } else if (tiles(64) <= 2 * kCUs) {
         launch_tiles<T, T, 64, 64, 2, 2, 4>(g, 1, s);
     } else if (tiles(128) <= kCUs) {
-        launch_tiles<T, T, 128, 128, 2, 2, 3>(g, 1, s);
+        launch_tiles<T, T, 128, 128, 2, 4, 3>(g, 1, s);
     } else if (tiles(256) < kCUs * 3 / 4) {
         launch_tiles<T, T, 128, 128, 2, 2, 2>(g, 1, s);
     } else {
