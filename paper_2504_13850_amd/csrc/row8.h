@@ -13,18 +13,20 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 // Eight values of a row.  NT: past the caches, for what a 256 MB last-level cache would not keep.
 template <class T, bool NT>
 struct Eight {
-    u32x4 u[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p, int n, bool vec) {
+    static constexpr int PIECES = sizeof(T) / 2, PER = 8 / PIECES;  // of 16 bytes
+    u32x4 u[PIECES];
+    // The first n of eight; vec: all of them.  `step`: where the second four of 32-bit values begin.
+    __device__ __forceinline__ void load(const T* p, int n, bool vec, int step = 4) {
         if (vec) {
 #pragma unroll
-            for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
-                const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p) + c;
+            for (int c = 0; c < PIECES; ++c) {
+                const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p + c * step);
                 u[c] = NT ? __builtin_nontemporal_load(q) : *q;
             }
         } else {
             T v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : T(0);
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e + (e / PER) * (step - 4)] : T(0);
             __builtin_memcpy(u, v, sizeof(u));
         }
     }
@@ -40,16 +42,16 @@ struct Eight {
         for (int e = 0; e < 8; ++e) v[e] = e == place ? x : v[e];
         __builtin_memcpy(u, v, sizeof(u));
     }
-    __device__ __forceinline__ static void store(T* p, const float* x, int n, bool vec) {
-        u32x4 w[sizeof(T) / 2];
+    __device__ __forceinline__ static void store(T* p, const float* x, int n, bool vec, int step = 4) {
+        u32x4 w[PIECES];
         if constexpr (sizeof(T) == 2)
             w[0] = u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])};
         else
             __builtin_memcpy(w, x, sizeof(w));
         if (vec) {
 #pragma unroll
-            for (int c = 0; c < (int)sizeof(T) / 2; ++c) {
-                u32x4_any* q = reinterpret_cast<u32x4_any*>(p) + c;
+            for (int c = 0; c < PIECES; ++c) {
+                u32x4_any* q = reinterpret_cast<u32x4_any*>(p + c * step);
                 if (NT) __builtin_nontemporal_store(w[c], q);
                 else *q = w[c];
             }
@@ -58,7 +60,7 @@ struct Eight {
             __builtin_memcpy(v, w, sizeof(w));
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < n) p[e] = v[e];
+                if (e < n) p[e + (e / PER) * (step - 4)] = v[e];
         }
     }
 };

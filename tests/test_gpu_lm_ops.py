@@ -80,7 +80,8 @@ LAYOUTS = [(0, 0), (3, 1)]
 EMBED = [(1, 1, 1), (1, 7, 3), (5, 8, 2), (33, 130, 32), (1203, 128, 32), (300, 77, 5000), (4096, 64, 1), (4097, 20, 600),
          (9000, 24, 40000), (20000, 40, 70), (70000, 8, 1200), (17000, 9, 2200000),
          (1024, 300, 5), (1024, 129, 1), (1025, 64, 900), (700, 16, 100003), (2048, 136, 40), (2, 9, 200000),
-         (512, 130, 3), (500, 264, 1), (512, 40, 300), (513, 40, 300)]
+         (512, 130, 3), (500, 264, 1), (512, 40, 300), (513, 40, 300),
+         (600, 2051, 70), (530, 1481, 12), (515, 4099, 9), (514, 2053, 3)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -113,6 +114,30 @@ def test_embed(dtype, rows, cols, vocab):
                 assert torch.equal(dtable.t[still].view(torch.uint8), before[still].view(torch.uint8))
             assert dtable.untouched()
         assert out.untouched()
+
+
+@pytest.mark.parametrize("dtype,rows,cols,vocab", [("f32", 33000, 2051, 600), ("f32", 9000, 1480, 40000),
+                                                   ("bf16", 66000, 2051, 600), ("bf16", 9000, 1480, 82000)])
+def test_embed_past_the_caches(dtype, rows, cols, vocab):
+    """More than 256 MB of rows or of table, against sums in 64 bits."""
+    torch = torch_cuda()
+    announce(f"embed past the caches {dtype} {rows} rows of {cols}, vocab {vocab}")
+    for pad, shift in LAYOUTS:
+        tokens = torch.randint(-1, vocab + 1, (rows,), device="cuda", dtype=torch.int32)
+        table, dout = Mat(vocab, cols, dtype, pad, shift, _normal(1, vocab, cols)), Mat(rows, cols, dtype, pad, shift, _normal(2, rows, cols))
+        out, dtable = Mat(rows, cols, dtype, pad, shift), Mat(vocab, cols, dtype, pad, shift)
+        A.fo_embed_fwd(tokens, table.t, out.t, scale=0.5)  # exact
+        inside = (tokens >= 0) & (tokens < vocab)
+        at = tokens[inside].long()
+        assert torch.equal(out.t[inside], table.t[at] * 0.5) and (out.t[~inside] == 0).all() and out.untouched()
+        A.fo_embed_bwd(tokens, dout.t, dtable.t, scale=0.5, workspace=_ws(A.fo_embed_workspace(rows, cols, vocab)))
+        terms = 0.5 * dout.t[inside].double()
+        zero = torch.zeros((vocab, cols), dtype=torch.float64, device="cuda")
+        want, size = zero.index_add(0, at, terms), zero.index_add(0, at, terms.abs())
+        count = torch.bincount(at, minlength=vocab)[:, None]
+        off = (dtable.t.double() - want).abs() > HALF[dtype] * want.abs() * (1 + 2 ** -8) + (count + 2) * F * size
+        assert not off.any(), f"{int(off.sum())} values off, first at {off.nonzero()[0].tolist()}"
+        assert dtable.untouched()
 
 
 def test_embed_without_rows():
