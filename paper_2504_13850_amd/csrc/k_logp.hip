@@ -106,10 +106,14 @@ __device__ __forceinline__ void add_chunk(const Eight<T, false>& x, Factor c, Pa
     float m = p.m;
 #pragma unroll
     for (int e = 0; e < 8; ++e) m = fmaxf(m, x.at(e));
-    float s = p.s * term(p.m, m, c);
+    float s[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += term(x.at(e), m, c);
-    p = {m, s};
+    for (int e = 0; e < 8; ++e) s[e] = term(x.at(e), m, c);
+#pragma unroll
+    for (int k = 4; k; k /= 2)  // one addition a chunk to what a thread has: a few threads' rows are as exact as many's
+#pragma unroll
+        for (int e = 0; e < k; ++e) s[e] += s[e + k];
+    p = {m, fmaf(p.s, term(p.m, m, c), s[0])};
 }
 
 constexpr int FLY = 4;  // chunks of a thread in flight
@@ -188,20 +192,21 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
 }
 
 // XENT: weight is minus the gradient by logp, and logp becomes the loss.  NT: past the caches.
-template <class T, bool XENT, bool NT>
+template <class T, int TPR, bool XENT, bool NT>
 __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, float* __restrict__ loss) {
-    const int64_t row = block_of();
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)block_of() * (256 / TPR) + threadIdx.x / TPR;
     if (row >= a.rows) return;
     const int target = a.targets[row], chunks = (a.vocab + 7) / 8;
     const bool there = target >= 0 && target < a.vocab;
     const float logp = a.logp[row], lse = a.lse[row];
-    if (XENT && blockIdx.z == 0 && threadIdx.x == 0) loss[row] = there ? -logp : 0.f;
+    if (XENT && blockIdx.z == 0 && t == 0) loss[row] = there ? -logp : 0.f;
     const T* x = (const T*)a.logits + row * a.ld;
     T* y = (T*)a.dlogits + row * a.dlogits_ld;
     const bool none = !there || lse == -INFINITY;
     const float g = none ? 0.f : (XENT ? -a.weight[row] : a.weight[row]) * a.scale;
     const float own = none ? 0.f : g * -expm1f(logp);
-    for (int c = blockIdx.z * 256 + threadIdx.x; c < chunks; c += gridDim.z * 256) {
+    for (int c = blockIdx.z * TPR + t; c < chunks; c += gridDim.z * TPR) {
         const int c0 = c * 8, n = min(8, a.vocab - c0);
         float d[8] = {};
         if (!none) {
@@ -292,39 +297,56 @@ int64_t part_bytes(int64_t rows, int32_t vocab) {
     return n > 1 ? cdiv(rows * n * (int64_t)sizeof(Part), 16) * 16 : 0;
 }
 
+template <class T, int TPR>
+void launch_fwd(const LogpArgs& a, hipStream_t s) {
+    constexpr int THREADS = TPR < 256 ? 256 : TPR;
+    logp_fwd_kernel<T, TPR, false><<<grid_of(cdiv(a.rows, THREADS / TPR)), THREADS, 0, s>>>(a, nullptr, 1);
+}
+// Short rows take few threads, for the logarithms in 64 bits take a wave as long whether one lane or 16 have a row
+// (bf16, 165000 rows of 128: 4 threads 17 us, 16 30, 64 108; 12000 of 4096: 16 threads 22, 64 24, 256 33), unless there
+// are too few rows to fill the chip so (500 rows of 1000: 4 threads 11.0, 64 6.0).
 template <class T>
 fo_status fwd(const LogpArgs& a, void* ws, hipStream_t s) {
     const int n = slices_of(a.rows, a.vocab);
+    const auto narrow = [&](int team, int32_t most) { return a.vocab <= (a.rows * team >= 1 << 16 ? most : 16 * team); };
     if (n > 1) {
         logp_fwd_kernel<T, 256, true><<<grid_of(a.rows * n), 256, 0, s>>>(a, (Part*)ws, n);
         FO_LAUNCHED();
         logp_join_kernel<T><<<grid_of(a.rows), 64, 0, s>>>(a, (const Part*)ws, n);
-    } else if (a.vocab <= 2048) {
-        logp_fwd_kernel<T, 64, false><<<grid_of(cdiv(a.rows, 4)), 256, 0, s>>>(a, nullptr, 1);
-    } else if (a.vocab <= 8192 || a.rows >= kWgs) {
-        logp_fwd_kernel<T, 256, false><<<grid_of(a.rows), 256, 0, s>>>(a, nullptr, 1);
-    } else {
-        logp_fwd_kernel<T, 1024, false><<<grid_of(a.rows), 1024, 0, s>>>(a, nullptr, 1);
-    }
+    } else if (narrow(4, 512)) launch_fwd<T, 4>(a, s);
+    else if (narrow(16, 4096)) launch_fwd<T, 16>(a, s);
+    else if (narrow(64, 8192)) launch_fwd<T, 64>(a, s);
+    else if (a.vocab <= 8192 || a.rows >= kWgs) launch_fwd<T, 256>(a, s);
+    else launch_fwd<T, 1024>(a, s);
     FO_LAUNCHED();
     return FO_OK;
-}
-
-// Workgroups along the vocabulary: one for each 16384 logits of a row, eight chunks a thread.
-dim3 bwd_grid(const LogpArgs& a) {
-    dim3 g = grid_of(a.rows);
-    g.z = (unsigned)std::min<int64_t>(cdiv(a.vocab, 16384), 65535);
-    return g;
 }
 
 // Logits and gradient that no cache keeps: a step of 5565 rows of 32000 bf16 takes 182 us with the gradient's loads and
 // stores past the caches, 232 through them.
 bool past_caches(const LogpArgs& a, int size) { return 2 * a.rows * a.vocab * size > int64_t(256) << 20; }
 
+template <class T, int TPR, bool XENT>
+void launch_bwd(const LogpArgs& a, float* loss, hipStream_t s) {
+    dim3 g = grid_of(cdiv(a.rows, 256 / TPR));
+    g.z = (unsigned)std::min<int64_t>(cdiv(a.vocab, 16384), 65535);  // along the vocabulary: eight chunks a thread
+    if (past_caches(a, sizeof(T))) logp_bwd_kernel<T, TPR, XENT, true><<<g, 256, 0, s>>>(a, loss);
+    else logp_bwd_kernel<T, TPR, XENT, false><<<g, 256, 0, s>>>(a, loss);
+}
+// A team about as wide as a row: 165000 rows of 128 bf16 16 us with 8 threads a row, 122 with 256; 50000 of 1024 34 with
+// 32 and 50.
 template <class T, bool XENT>
 fo_status bwd(const LogpArgs& a, float* loss, hipStream_t s) {
-    if (past_caches(a, sizeof(T))) logp_bwd_kernel<T, XENT, true><<<bwd_grid(a), 256, 0, s>>>(a, loss);
-    else logp_bwd_kernel<T, XENT, false><<<bwd_grid(a), 256, 0, s>>>(a, loss);
+    const int64_t bytes = a.vocab * (int64_t)sizeof(T);
+    if constexpr (XENT) {  // of rows that xent_kernel does not hold
+        if (bytes <= 256) launch_bwd<T, 8, XENT>(a, loss, s);
+        else launch_bwd<T, 256, XENT>(a, loss, s);
+    } else {
+        if (bytes <= 256) launch_bwd<T, 8, XENT>(a, loss, s);
+        else if (bytes <= 2048) launch_bwd<T, 32, XENT>(a, loss, s);
+        else if (bytes <= 4096) launch_bwd<T, 64, XENT>(a, loss, s);
+        else launch_bwd<T, 256, XENT>(a, loss, s);
+    }
     FO_LAUNCHED();
     return FO_OK;
 }
@@ -333,8 +355,12 @@ fo_status bwd(const LogpArgs& a, float* loss, hipStream_t s) {
 // pass and the gradient.
 bool held(int32_t vocab) { return vocab >= 8 && vocab <= kOneWg; }
 
-template <class T, int TPR, int NC>
+// The narrowest of the teams and chunks that holds a row: registers that hold nothing cost (bf16, 165000 rows of 128: 4
+// threads 20 us, 8 30, 64 122; 16400 rows of 9000: 512 threads with three chunks 119, with four 158, 1024 with four 282).
+template <class T, int TPR, int NC, int... REST>
 void launch_xent(const LogpArgs& a, hipStream_t s) {
+    if constexpr (sizeof...(REST) != 0)
+        if (a.vocab > TPR * NC * 8) return launch_xent<T, REST...>(a, s);
     constexpr int THREADS = TPR < 256 ? 256 : TPR;
     const dim3 g = grid_of(cdiv(a.rows, THREADS / TPR));
     if (past_caches(a, sizeof(T))) xent_kernel<T, TPR, NC, true><<<g, THREADS, 0, s>>>(a);
@@ -350,10 +376,7 @@ fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
         const fo_status st = fwd<T>(b, ws, s);
         return st != FO_OK ? st : bwd<T, true>(b, a.logp, s);
     }
-    if (a.vocab <= 1024) launch_xent<T, 64, 2>(a, s);
-    else if (a.vocab <= 8192) launch_xent<T, 256, 4>(a, s);
-    else if (a.vocab <= 32768) launch_xent<T, 1024, 4>(a, s);
-    else launch_xent<T, 1024, 8>(a, s);
+    launch_xent<T, 4, 4, 8, 4, 16, 4, 32, 4, 64, 4, 256, 2, 256, 3, 256, 4, 512, 3, 512, 4, 1024, 3, 1024, 4, 1024, 6, 1024, 8>(a, s);
     FO_LAUNCHED();
     return FO_OK;
 }

@@ -364,7 +364,9 @@ def test_gemm_f8_nan_keeps_to_its_row():
 
 # ------------------------------------------------------------------ log probabilities
 LOGP = [(1, 1), (1, 2), (5, 7), (3, 8), (70, 33), (300, 1000), (9, 1025), (600, 2049), (4, 8192), (520, 8200), (600, 16384),
-        (3, 32000), (530, 32001), (2, 50000), (515, 66001), (1, 128000), (513, 131073), (1, 300001)]
+        (3, 32000), (530, 32001), (2, 50000), (515, 66001), (1, 128000), (513, 131073), (1, 300001),
+        (100, 127), (100, 129), (50, 256), (40, 257), (40, 511), (30, 513), (20, 2047), (10, 4097), (10, 6145), (5, 12290),
+        (3, 16386), (3, 24579), (2, 49155), (16400, 130), (16390, 512), (20000, 60), (4100, 1500), (1030, 5003)]
 
 
 def _logits(dtype, rows, vocab, pad, shift, seed=1):
