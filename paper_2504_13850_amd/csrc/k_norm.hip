@@ -21,15 +21,17 @@ struct Shape {
     static constexpr int64_t COLS = int64_t(TPR_) * NC_ * 8;
 };
 
-// The narrowest of the shapes that holds a row; false for rows that none holds.
+// The narrowest of the shapes that holds a row, up to `most` columns; false for rows that none holds.
 template <class F>
-bool with_shape(int32_t cols, F f) {
+bool with_shape(int32_t cols, int64_t most, F f) {
+    if (cols > most) return false;
     if (cols <= Shape<256, 16, 1>::COLS) f(Shape<256, 16, 1>{});
     else if (cols <= Shape<256, 64, 1>::COLS) f(Shape<256, 64, 1>{});
     else if (cols <= Shape<256, 64, 2>::COLS) f(Shape<256, 64, 2>{});
     else if (cols <= Shape<256, 256, 1>::COLS) f(Shape<256, 256, 1>{});
     else if (cols <= Shape<256, 256, 2>::COLS) f(Shape<256, 256, 2>{});
-    else if (cols <= Shape<256, 256, 4>::COLS) f(Shape<256, 256, 4>{});
+    else if (cols <= Shape<256, 256, 3>::COLS) f(Shape<256, 256, 3>{});
+    else if (cols <= Shape<1024, 1024, 1>::COLS) f(Shape<1024, 1024, 1>{});
     else if (cols <= Shape<1024, 1024, 2>::COLS) f(Shape<1024, 1024, 2>{});
     else if (cols <= Shape<1024, 1024, 4>::COLS) f(Shape<1024, 1024, 4>{});
     else return false;
@@ -184,7 +186,7 @@ bool past_caches(int64_t rows, int32_t cols) { return 4 * rows * cols * (int64_t
 
 template <class T, int OUT>
 fo_status fwd(const NormArgs& a, hipStream_t s) {
-    const bool held = with_shape(a.cols, [&](auto shape) {
+    const bool held = with_shape(a.cols, INT32_MAX, [&](auto shape) {
         using S = decltype(shape);
         const dim3 g = grid_of(cdiv(a.rows, S::RPW));
         if (OUT == kNorm && past_caches<T>(a.rows, a.cols)) norm_kernel<T, S, OUT, OUT == kNorm><<<g, S::THREADS, 0, s>>>(a);
@@ -200,13 +202,19 @@ fo_status fwd_any(NormOut out, const NormArgs& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ backward
-// Workgroups, and parts of the weight's gradient: each takes every so many-th row.  Two rows a team before there are more
-// than 512 (4096 rows of 768: 19.6 us forward and backward, 21.1 with one), and no more than 1024.
+// Columns that the registers of a workgroup hold with the weight's gradient (3000 rows of 20000 bf16: 161 us through the
+// long rows' kernels, 320 with what spills; fp32, 2000 rows without residual: 188 and 316).
+constexpr int64_t kBwdCols = Shape<1024, 1024, 2>::COLS;
+
+// Workgroups, and parts of the weight's gradient: each takes every so many-th row.  As many as the chip has room for:
+// parts are written and read once more (bf16 with residual: 2048 rows of 16384 58 us with 256 parts, 75 with 512, 104
+// with 1024; 4096 of 4096 31 with 512, 36 with 1024).  Of short rows more, two rows a team (100000 of 64: 19 us with
+// 1024, 26 with 512).  Long rows: 1024 workgroups along rows and columns.
 int64_t bwd_parts(int64_t rows, int32_t cols) {
-    int rpw = 1;
-    with_shape(cols, [&](auto shape) { rpw = decltype(shape)::RPW; });
+    int64_t rpw = 1, most = std::max<int64_t>(1, 1024 / cdiv(cols, 2048));
+    with_shape(cols, kBwdCols, [&](auto shape) { rpw = decltype(shape)::RPW, most = decltype(shape)::THREADS == 1024 ? 256 : 512; });
     const int64_t n = cdiv(rows, rpw);
-    return n <= 512 ? std::max<int64_t>(1, n) : std::min<int64_t>(1024, std::max<int64_t>(512, n / 2));
+    return std::max<int64_t>(1, std::min(n, cols > 512 ? most : std::min<int64_t>(1024, std::max(most, n / 2))));
 }
 
 // 64 columns of dw, all rows: eight threads along the columns, the others' sums joined in order.
@@ -249,42 +257,55 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a, int
         dw_columns<T, S::THREADS>(a, (int)blockIdx.x - rows_wgs, sums);
         return;
     }
+    // Where a whole workgroup of 1024 has a row, the next one's loads are in flight if the registers hold both.
+    constexpr bool NEXT = S::TPR == 1024 && S::NC == 1;
     const int t = threadIdx.x % S::TPR, ty = threadIdx.x / S::TPR;
     float w[S::NC][8], dw[S::NC][8] = {};
 #pragma unroll
     for (int c = 0; c < S::NC; ++c) load_w<T>(a.w, (t + c * S::TPR) * 8, min(8, a.cols - (t + c * S::TPR) * 8), w[c]);
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * S::RPW + ty; row < a.rows; row += (int64_t)rows_wgs * S::RPW) {
+    struct Operands {
         Eight<T, NT> dy[S::NC], h[S::NC], dr[S::NC];
-        const float r = a.rstd[row];
-        float dot = 0.f;
+        float r;
+    };
+    const auto load = [&](int64_t row, Operands& o) {
+        o.r = a.rstd[row];
 #pragma unroll
         for (int c = 0; c < S::NC; ++c) {
             const int c0 = (t + c * S::TPR) * 8, n = min(8, a.cols - c0);
-            dy[c].load((const T*)a.dy + row * a.dy_ld + c0, n, n == 8);
-            h[c].load((const T*)a.h + row * a.h_ld + c0, n, n == 8);
-            if (a.dres) dr[c].load((const T*)a.dres + row * a.dres_ld + c0, n, n == 8);
+            o.dy[c].load((const T*)a.dy + row * a.dy_ld + c0, n, n == 8);
+            o.h[c].load((const T*)a.h + row * a.h_ld + c0, n, n == 8);
+            if (a.dres) o.dr[c].load((const T*)a.dres + row * a.dres_ld + c0, n, n == 8);
         }
+    };
+    const int64_t row0 = (int64_t)blockIdx.x * S::RPW + ty, each = (int64_t)rows_wgs * S::RPW;
+    Operands o, next;
+    if (NEXT && row0 < a.rows) load(row0, o);
+    int turn = 0;
+    for (int64_t row = row0; row < a.rows; row += each) {
+        if (!NEXT) load(row, o);
+        else if (row + each < a.rows) load(row + each, next);
+        float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dot += dy[c].at(e) * w[c][e] * h[c].at(e);
+            for (int e = 0; e < 8; ++e) dot += o.dy[c].at(e) * w[c][e] * o.h[c].at(e);
         dot = team<S::TPR>(dot, lds[turn & 1], Add());
         ++turn;
-        const float k = r * r * (dot / (float)a.cols);
+        const float r = o.r, k = r * r * (dot / (float)a.cols);
 #pragma unroll
         for (int c = 0; c < S::NC; ++c) {
             const int c0 = (t + c * S::TPR) * 8, n = min(8, a.cols - c0);
             float dx[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float g = dy[c].at(e), x = h[c].at(e);
+                const float g = o.dy[c].at(e), x = o.h[c].at(e);
                 dx[e] = r * (g * w[c][e] - x * k);
-                if (a.dres) dx[e] += dr[c].at(e);
+                if (a.dres) dx[e] += o.dr[c].at(e);
                 dw[c][e] += g * (x * r);
             }
             if (n > 0) Eight<T, NT>::store((T*)a.dx + row * a.dx_ld + c0, dx, n, n == 8);
         }
+        if (NEXT) o = next;
     }
     if (FEW || !a.part) return;
 #pragma unroll
@@ -366,15 +387,15 @@ __global__ void __launch_bounds__(256) norm_dw_long_kernel(NormBwdArgs a, int pa
 }
 
 // Up to 512 rows dw is cheaper read for than joined in a second launch (a pass forward and backward, bf16: 4 rows of 768
-// 7.6 us and 10.3, 512 of 8192 20 and 35; 1024 of 768 14 and 12), unless dx lies over what it reads.
+// 7.6 us and 10.3, 512 of 8192 23 and 32; 1024 of 768 14 and 12), unless dx lies over what it reads.
 constexpr int64_t kFewRows = 512;
 template <class T>
 fo_status bwd(const NormBwdArgs& args, void* dw, hipStream_t s) {
     NormBwdArgs a = args;
     const int parts = (int)bwd_parts(a.rows, a.cols);
-    const bool few = dw && a.rows <= kFewRows && a.rows > 0 && a.cols <= Shape<1024, 1024, 4>::COLS && a.dx != a.dy && a.dx != a.h;
+    const bool few = dw && a.rows <= kFewRows && a.rows > 0 && a.cols <= kBwdCols && a.dx != a.dy && a.dx != a.h;
     if (a.rows) {
-        const bool held = with_shape(a.cols, [&](auto shape) {
+        const bool held = with_shape(a.cols, kBwdCols, [&](auto shape) {
             using S = decltype(shape);
             if (few) {
                 a.dw = dw;

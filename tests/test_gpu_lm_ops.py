@@ -154,7 +154,8 @@ def test_embed_without_rows():
 
 # ------------------------------------------------------------------ RMS norm
 NORM = [(1, 1), (3, 5), (1, 8), (17, 100), (70, 128), (5, 129), (9, 768), (300, 513), (4, 1025), (3, 2050), (6, 4096),
-        (2, 4099), (3, 8200), (2, 16385), (2, 32771), (2100, 64), (1500, 1000)]
+        (2, 4099), (3, 8200), (2, 16385), (2, 32771), (2100, 64), (1500, 1000),
+        (2, 6144), (3, 6145), (2, 8191), (520, 4101), (800, 6150), (600, 9001), (530, 16388), (1000, 1023), (70, 20005)]
 
 
 def _norm_slack(cols):
@@ -214,6 +215,21 @@ def test_norm_in_place(cols):
     assert torch.equal(r2, y) and torch.equal(x2, h)
     dy, dres, dx, dw = _normal(4, 5, cols), _normal(5, 5, cols), torch.empty_like(x), torch.empty_like(w)
     ws = _ws(A.fo_rmsnorm_workspace(5, cols))
+    A.fo_rmsnorm_bwd(dy, h, w, rstd, dx, dw=dw, dres=dres, workspace=ws)
+    for over in range(3):
+        v, dw2 = [dy.clone(), dres.clone(), h.clone()], torch.empty_like(w)
+        A.fo_rmsnorm_bwd(v[0], v[2], w, rstd, v[over], dw=dw2, dres=v[1], workspace=ws)
+        assert torch.equal(v[over], dx) and torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("rows,cols", [(600, 6300), (530, 5001), (520, 18000)])
+def test_norm_backward_of_many_rows_in_place(rows, cols):
+    torch = torch_cuda()
+    announce(f"norm backward in place, {rows} rows of {cols}")
+    dy, dres, h, w = (_normal(s, rows, cols) for s in (1, 2, 3, 4))
+    w, rstd = w[0].contiguous(), _normal(5, rows).abs()
+    dx, dw = torch.empty_like(dy), torch.empty_like(w)
+    ws = _ws(A.fo_rmsnorm_workspace(rows, cols))
     A.fo_rmsnorm_bwd(dy, h, w, rstd, dx, dw=dw, dres=dres, workspace=ws)
     for over in range(3):
         v, dw2 = [dy.clone(), dres.clone(), h.clone()], torch.empty_like(w)
