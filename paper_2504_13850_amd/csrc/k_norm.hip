@@ -96,14 +96,26 @@ __global__ void __launch_bounds__(S::THREADS) norm_kernel(NormArgs a) {
     const int64_t row = (int64_t)block_of() * S::RPW + threadIdx.x / S::TPR;
     if (row >= a.rows) return;  // whole teams, and whole workgroups where a team needs a barrier
     float h[S::NC][8], w[S::NC][8], ss = 0.f, top = 0.f;
+    Eight<T, NT> x[S::NC], res[S::NC];
+    Eight<T, false> u[S::NC];
 #pragma unroll
     for (int c = 0; c < S::NC; ++c) {
-        const int c0 = (t + c * S::TPR) * 8, n = min(8, a.cols - c0);
+        const int c0 = (t + c * S::TPR) * 8;
+        if (c0 >= a.cols) continue;
+        x[c].load_row((const T*)a.x + row * a.x_ld, c0, a.cols);
+        if (a.res) res[c].load_row((const T*)a.res + row * a.res_ld, c0, a.cols);
+        if (OUT != kQuantF8 && a.w) u[c].load_row((const T*)a.w, c0, a.cols);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[c][e] = w[c][e] = 0.f;
-        if (n > 0) {
-            load_h<T, NT>(a, row, c0, n, h[c]);
-            if (OUT != kQuantF8) load_w<T>(a.w, c0, n, w[c]);
+    for (int c = 0; c < S::NC; ++c) {
+        const int n = min(8, a.cols - (t + c * S::TPR) * 8);
+        x[c].fit(n, a.cols);
+        if (a.res) res[c].fit(n, a.cols);
+        if (OUT != kQuantF8 && a.w) u[c].fit(n, a.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            h[c][e] = n <= 0 ? 0.f : a.res ? x[c].at(e) + res[c].at(e) : x[c].at(e);
+            w[c][e] = n <= 0 ? 0.f : OUT != kQuantF8 && a.w ? u[c].at(e) : 1.f;
         }
     }
 #pragma unroll
@@ -259,6 +271,9 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a, int
     }
     // Where a whole workgroup of 1024 has a row, the next one's loads are in flight if the registers hold both.
     constexpr bool NEXT = S::TPR == 1024 && S::NC == 1;
+    // Row's ends by load_row in 16 bits (5247 rows of 6845 87 us, 109 by single elements); in 32 the registers that fit()
+    // needs cost more (12020 rows of 753 34 and 31).
+    constexpr bool FIT = sizeof(T) == 2;
     const int t = threadIdx.x % S::TPR, ty = threadIdx.x / S::TPR;
     float w[S::NC][8], dw[S::NC][8] = {};
 #pragma unroll
@@ -272,9 +287,14 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a, int
 #pragma unroll
         for (int c = 0; c < S::NC; ++c) {
             const int c0 = (t + c * S::TPR) * 8, n = min(8, a.cols - c0);
-            o.dy[c].load((const T*)a.dy + row * a.dy_ld + c0, n, n == 8);
-            o.h[c].load((const T*)a.h + row * a.h_ld + c0, n, n == 8);
-            if (a.dres) o.dr[c].load((const T*)a.dres + row * a.dres_ld + c0, n, n == 8);
+            const auto get = [&](const void* p, int64_t ld, Eight<T, NT>& x) {
+                if (FIT) x.load_row((const T*)p + row * ld, c0, a.cols);
+                else x.load((const T*)p + row * ld + c0, n, n == 8);
+            };
+            if (FIT && n <= 0) continue;
+            get(a.dy, a.dy_ld, o.dy[c]);
+            get(a.h, a.h_ld, o.h[c]);
+            if (a.dres) get(a.dres, a.dres_ld, o.dr[c]);
         }
     };
     const int64_t row0 = (int64_t)blockIdx.x * S::RPW + ty, each = (int64_t)rows_wgs * S::RPW;
@@ -286,9 +306,17 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(NormBwdArgs a, int
         else if (row + each < a.rows) load(row + each, next);
         float dot = 0.f;
 #pragma unroll
-        for (int c = 0; c < S::NC; ++c)
+        for (int c = 0; c < S::NC; ++c) {
+            const int n = min(8, a.cols - (t + c * S::TPR) * 8);
+            if (FIT) {
+                o.dy[c].fit(n, a.cols);
+                o.h[c].fit(n, a.cols);
+                if (a.dres) o.dr[c].fit(n, a.cols);
+            }
+            if (!FIT || n > 0)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dot += o.dy[c].at(e) * w[c][e] * o.h[c].at(e);
+                for (int e = 0; e < 8; ++e) dot += o.dy[c].at(e) * w[c][e] * o.h[c].at(e);
+        }
         dot = team<S::TPR>(dot, lds[turn & 1], Add());
         ++turn;
         const float r = o.r, k = r * r * (dot / (float)a.cols);
