@@ -41,6 +41,17 @@ __device__ __forceinline__ Mine mine_of(int32_t cols, int tx) {
     return {c + t * 4, t * 4 >= step ? 0 : second > 0 ? 4 + min(4, second) : min(4, w - t * 4), step};
 }
 
+// A thread's columns of a row, in two steps: the loads of several rows, then the row's end put in place (16 bits).
+template <class T, bool NT>
+__device__ __forceinline__ void load_mine(Eight<T, NT>& x, const T* row, Mine m, int32_t cols) {
+    if (sizeof(T) == 2) x.load_row(row, (int)m.c0, cols);
+    else x.load(row + m.c0, m.n, m.n == 8, m.step);
+}
+template <class T, bool NT>
+__device__ __forceinline__ void fit_mine(Eight<T, NT>& x, Mine m, int32_t cols) {
+    if (sizeof(T) == 2) x.fit(m.n, cols);
+}
+
 constexpr int64_t kPastCaches = int64_t(256) << 20;
 
 // ------------------------------------------------------------------ forward
@@ -49,9 +60,9 @@ constexpr int FWD_FLY = 4;  // rows of a team in flight
 template <class T, bool NT>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tx) {
     const int ty = threadIdx.x >> tx, teams = 256 >> tx;
-    const auto [c0, n, step] = mine_of<T>(a.cols, tx);
+    const Mine m = mine_of<T>(a.cols, tx);
     const int64_t r0 = (int64_t)block_of() * teams * FWD_FLY + ty;
-    if (n <= 0) return;
+    if (m.n <= 0) return;
     int token[FWD_FLY];
     Eight<T, false> x[FWD_FLY];
 #pragma unroll
@@ -59,7 +70,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tx) {
 #pragma unroll
     for (int k = 0; k < FWD_FLY; ++k) {
         if ((uint32_t)token[k] < (uint32_t)a.vocab)
-            x[k].load((const T*)a.table + token[k] * a.table_ld + c0, n, n == 8, step);
+            load_mine(x[k], (const T*)a.table + token[k] * a.table_ld, m, a.cols);
         else
             x[k] = {};
     }
@@ -67,12 +78,13 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(EmbedArgs a, int tx) {
     for (int k = 0; k < FWD_FLY; ++k) {
         if (r0 + k * teams >= a.rows) continue;
         float y[8];
+        fit_mine(x[k], m, a.cols);
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[k].at(e) * a.scale;
         if ((uint32_t)token[k] >= (uint32_t)a.vocab)
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = 0.f;
-        Eight<T, NT>::store((T*)a.out + (r0 + k * teams) * a.out_ld + c0, y, n, n == 8, step);
+        Eight<T, NT>::store((T*)a.out + (r0 + k * teams) * a.out_ld + m.c0, y, m.n, m.n == 8, m.step);
     }
 }
 
@@ -353,7 +365,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, const Entry
         for (int u = 0; u < SUM_FLY; ++u) e[u] = i + u < i1 ? own(i + u) : make_uint2(~0u, 0u);
 #pragma unroll
         for (int u = 0; u < SUM_FLY; ++u)
-            if (e[u].x < vocab) x[u].load((const T*)a.dout + (int64_t)e[u].y * a.dout_ld + m.c0, m.n, m.n == 8, m.step);
+            if (e[u].x < vocab) load_mine(x[u], (const T*)a.dout + (int64_t)e[u].y * a.dout_ld, m, a.cols);
 #pragma unroll
         for (int u = 0; u < SUM_FLY; ++u) {
             if (i + u >= i1 || e[u].x >= vocab) break;
@@ -365,6 +377,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(EmbedArgs a, const Entry
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum[k] = 0.f;
             }
+            fit_mine(x[u], m, a.cols);
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum[k] += x[u].at(k);
         }
