@@ -376,7 +376,8 @@ fo_status xent(const LogpArgs& a, void* ws, hipStream_t s) {
         const fo_status st = fwd<T>(b, ws, s);
         return st != FO_OK ? st : bwd<T, true>(b, a.logp, s);
     }
-    launch_xent<T, 4, 4, 8, 4, 16, 4, 32, 4, 64, 4, 256, 2, 256, 3, 256, 4, 512, 3, 512, 4, 1024, 3, 1024, 4, 1024, 6, 1024, 8>(a, s);
+    launch_xent<T, 4, 4, 8, 4, 16, 4, 32, 4, 64, 4, 256, 2, 256, 3, 256, 4, 512, 3, 512, 4, 1024, 3, 1024, 4, 1024, 6, 1024, 7,
+                1024, 8>(a, s);
     FO_LAUNCHED();
     return FO_OK;
 }
