@@ -307,9 +307,9 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(EmbedArgs a, 
 // ------------------------------------------------------------------ sums
 // Entries of a piece: short pieces where rows are few or narrow, so that teams fill the chip, and some thousand pieces at
 // most, for each takes a workgroup of the join (the gradient, bf16: 56548 rows of 101 in pieces of 16 35 us, of 64 54;
-// 65536 of 768 69 and 63; 200000 of 128 76 and 50).
+// 65536 of 2048 197 and 187, of 768 69 and 63; 200000 of 128 76 and 50).
 int piece_of(int64_t rows, int32_t cols) {
-    const int64_t most = 256 >> team_bits(cols) >= 8 ? 4096 : 2048;
+    const int64_t most = 256 >> team_bits(cols) >= 8 ? 4096 : 1536;
     int piece = 8;
     while (piece < 64 && cdiv(rows, piece) > most) piece *= 2;
     return piece;

@@ -191,8 +191,9 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(NormArgs a) {
     }
 }
 
-// Operands that no cache keeps: 16384 rows of 4096 bf16, a pass forward and backward 183 us with the loads past the
-// caches, which leaves h and y to the launches that read them, 216 through them (stores of h and y past them too: 197; of dx 180).
+// Operands that no cache keeps: 16384 rows of 4096 bf16, a pass forward and backward 166 us with the loads and
+// dx past the caches, which leaves h and y to the launches that read them, 203 through them (stores of h and y past them
+// too cost another 14).
 template <class T>
 bool past_caches(int64_t rows, int32_t cols) { return 4 * rows * cols * (int64_t)sizeof(T) > int64_t(256) << 20; }
 
