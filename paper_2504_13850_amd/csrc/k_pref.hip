@@ -55,7 +55,9 @@ __global__ void __launch_bounds__(THREADS) pref_kernel(PrefArgs p) {
     }
     const float d = (float)(reward[0] - reward[1]);
     if (threadIdx.x == 0) {
-        p.loss[pair] = (1.f - p.smooth) * softplus(-d) + p.smooth * softplus(d);
+        // a term without weight counts as 0 where it is infinite too
+        p.loss[pair] = (p.smooth < 1.f ? (1.f - p.smooth) * softplus(-d) : 0.f) +
+                       (p.smooth > 0.f ? p.smooth * softplus(d) : 0.f);
         p.reward[2 * pair] = (float)reward[0];
         p.reward[2 * pair + 1] = (float)reward[1];
     }
