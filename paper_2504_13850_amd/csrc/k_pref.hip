@@ -1,8 +1,9 @@
 // Preference loss: a workgroup a pair, one launch.
 //
 // Twelve bytes a row and a handful of operations a pair: the call costs its launch
-// and one pass of dependent loads.  Sums in fp64: answers are long, and the two
-// sums of a pair nearly cancel.
+// and one pass of dependent loads.  All in fp64 up to the results' one rounding:
+// answers are long, the two sums of a pair nearly cancel, and an error of d is a
+// relative one of the loss and of its gradient.
 #include "lm.h"
 
 namespace fo {
@@ -16,13 +17,6 @@ struct Rows {
 __device__ __forceinline__ Rows answer(const PrefArgs& p, int64_t q) {
     const int64_t lo = min(max((int64_t)p.begin[q], (int64_t)0), p.rows);
     return {lo, min(max((int64_t)p.end[q], lo), p.rows)};
-}
-
-// log(1 + exp(x)) and 1 / (1 + exp(-x)), neither overflowing.
-__device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
-__device__ __forceinline__ float sigma(float x) {
-    const float e = expf(-fabsf(x));
-    return (x >= 0.f ? 1.f : e) / (1.f + e);
 }
 
 __global__ void __launch_bounds__(THREADS) pref_kernel(PrefArgs p) {
@@ -41,31 +35,32 @@ __global__ void __launch_bounds__(THREADS) pref_kernel(PrefArgs p) {
         if ((threadIdx.x & 63) == 0) part[q][threadIdx.x >> 6] = sum[q];
     }
     __syncthreads();  // every row has been read: dlogp may lie over logp
-    double reward[2];
-    float each[2];
+    double reward[2], each[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         reward[q] = 0.0;
 #pragma unroll
         for (int k = 0; k < THREADS / 64; ++k) reward[q] += part[q][k];
         const int64_t n = at[q].hi - at[q].lo;
-        const double b = p.mean && n > 1 ? (double)p.beta / (double)n : (double)p.beta;
-        reward[q] *= b;
-        each[q] = (float)b;
+        each[q] = p.mean && n > 1 ? (double)p.beta / (double)n : (double)p.beta;
+        reward[q] *= each[q];
     }
-    const float d = (float)(reward[0] - reward[1]);
+    // log(1 + exp(+-d)) = max(+-d, 0) + log(1 + exp(-|d|)), 1 / (1 + exp(+-d)) from the same exponential: nothing overflows
+    const double d = reward[0] - reward[1], smooth = p.smooth, e = exp(-fabs(d));
     if (threadIdx.x == 0) {
+        const double both = log1p(e);
         // a term without weight counts as 0 where it is infinite too
-        p.loss[pair] = (p.smooth < 1.f ? (1.f - p.smooth) * softplus(-d) : 0.f) +
-                       (p.smooth > 0.f ? p.smooth * softplus(d) : 0.f);
+        p.loss[pair] = (float)((smooth < 1.0 ? (1.0 - smooth) * (fmax(-d, 0.0) + both) : 0.0) +
+                               (smooth > 0.0 ? smooth * (fmax(d, 0.0) + both) : 0.0));
         p.reward[2 * pair] = (float)reward[0];
         p.reward[2 * pair + 1] = (float)reward[1];
     }
     if (!p.dlogp) return;
-    const float slope = p.dloss * (p.smooth * sigma(d) - (1.f - p.smooth) * sigma(-d));
+    const double up = (d >= 0.0 ? 1.0 : e) / (1.0 + e), down = (d >= 0.0 ? e : 1.0) / (1.0 + e);
+    const double slope = (double)p.dloss * (smooth * up - (1.0 - smooth) * down);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const float g = (q ? -slope : slope) * each[q];
+        const float g = (float)((q ? -slope : slope) * each[q]);
         for (int64_t r = at[q].lo + threadIdx.x; r < at[q].hi; r += THREADS) p.dlogp[r] = g;
     }
 }

@@ -46,3 +46,29 @@ def test_pref_infinite_rewards(smooth):
     bound = 3 * F * abs(want)
     bound[30:40] = (12 + 2 * abs(dd)) * F * 0.125
     _near("dlogp", _np(d), want, np.nan_to_num(bound))
+
+
+@pytest.mark.parametrize("n,apart,beta,smooth,mean", [(1500, 0.04, 0.5, 0.0, False), (1500, -0.04, 0.5, 0.0, False),
+                                                      (900, 0.03, 0.5, 0.1, False), (2000, 0.3, 40.0, 0.0, True),
+                                                      (37, 0.2, 0.1, 0.5, False)])
+def test_pref_of_long_answers_keeps_its_bits(n, apart, beta, smooth, mean):
+    """Sums and functions in 64 bits, results rounded once.  The sums are off by at most n 2^-53 of their terms' sizes,
+    and loss and gradient by that, relative, for neither's logarithm is steeper than 1 in d."""
+    torch = torch_cuda()
+    announce(f"preference loss, answers of {n}")
+    for seed in range(4):
+        spans = [(0, n), (n, 2 * n + 3)]
+        logp, ref = -_normal(seed, 2 * n + 3).abs() * 2, -_normal(seed + 9, 2 * n + 3).abs() * 2
+        logp[:n] += apart + ref[:n] - logp[:n] + 0.01 * logp[:n]
+        logp[n:] += -apart + ref[n:] - logp[n:] + 0.01 * logp[n:]
+        loss, reward, d = torch.empty(1, device="cuda"), torch.empty(2, device="cuda"), torch.empty(2 * n + 3, device="cuda")
+        A.fo_pref_loss(logp, ref, _i32([0, n]), _i32([n, 2 * n + 3]), loss, reward, d, beta=beta, smooth=smooth, mean=mean,
+                       dloss=0.7)
+        b, sm = float(np.float32(beta)), float(np.float32(smooth))
+        wl, wr, wd, size, _ = R.pref(_np(logp), _np(ref), spans, b, sm, mean, float(np.float32(0.7)))
+        each = b / n if mean else b
+        off = 2 * (2 * n * 2.0 ** -53 * each * (abs(_np(logp)) + abs(_np(ref))).sum() + 2.0 ** -46)
+        assert off < F / 8
+        _near("reward", _np(reward), wr, (1 + 2 ** -8) * F * abs(wr) + off)
+        _near("loss", _np(loss), wl, (1 + 2 ** -8) * F * wl + off * wl)
+        _near("dlogp", _np(d), wd, (1 + 2 ** -8) * F * abs(wd) + off * size)
