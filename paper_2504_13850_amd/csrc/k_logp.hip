@@ -191,22 +191,39 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
     if (a.lse) a.lse[row] = r.y;
 }
 
+// Which of a row's chunks a launch of the gradient writes.  Over the logits themselves no other workgroup may lose the
+// target's logit before it has read it: all but its chunk in one launch, that chunk in the next.
+enum Chunks { kAll, kOthers, kTargets };
+
+// exp(z - lse) of every term is off by what lse lost when it was rounded, up to |lse| 2^-24 of itself: as long as logp is
+// the smaller of the two, z_t - logp says how much that was, to 2^-24 |logp| (logits around 100000: gradients off by
+// 3e-3, and by 1e-6 so).  One factor a row.
+__device__ __forceinline__ float lost_of(float zt, float scale, float logp, float lse) {
+    return fabsf(logp) < fabsf(lse) && lse - lse == 0.f ? expf(logp - fmaf(zt, scale, -lse)) : 1.f;
+}
+
 // XENT: weight is minus the gradient by logp, and logp becomes the loss.  NT: past the caches.
 template <class T, int TPR, bool XENT, bool NT>
-__global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, float* __restrict__ loss) {
+__global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, Chunks which, float* __restrict__ loss) {
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)block_of() * (256 / TPR) + threadIdx.x / TPR;
     if (row >= a.rows) return;
     const int target = a.targets[row], chunks = (a.vocab + 7) / 8;
     const bool there = target >= 0 && target < a.vocab;
     const float logp = a.logp[row], lse = a.lse[row];
-    if (XENT && blockIdx.z == 0 && t == 0) loss[row] = there ? -logp : 0.f;
     const T* x = (const T*)a.logits + row * a.ld;
     T* y = (T*)a.dlogits + row * a.dlogits_ld;
+    const float zt = there ? to_f(x[target]) : 0.f;
+    if (TPR > 64) __syncthreads();  // every wave has read it: dlogits may lie over the logits
+    if (XENT && which != kTargets && blockIdx.z == 0 && t == 0) loss[row] = there ? -logp : 0.f;
     const bool none = !there || lse == -INFINITY;
     const float g = none ? 0.f : (XENT ? -a.weight[row] : a.weight[row]) * a.scale;
-    const float own = none ? 0.f : g * -expm1f(logp);
-    for (int c = blockIdx.z * TPR + t; c < chunks; c += gridDim.z * TPR) {
+    const float own = none ? 0.f : g * -expm1f(logp), others = none ? 0.f : -g * lost_of(zt, a.scale, logp, lse);
+    const int mine = there ? target >> 3 : -1;
+    if (which == kTargets && (t || !there)) return;
+    const int first = which == kTargets ? mine : (int)blockIdx.z * TPR + t, last = which == kTargets ? mine + 1 : chunks;
+    for (int c = first; c < last; c += gridDim.z * TPR) {
+        if (which == kOthers && c == mine) continue;
         const int c0 = c * 8, n = min(8, a.vocab - c0);
         float d[8] = {};
         if (!none) {
@@ -214,7 +231,7 @@ __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, float* __rest
             u.load(x + c0, n, n == 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = -g * __builtin_amdgcn_exp2f(fmaf(u.at(e), a.scale, -lse) * kLog2e);
+                d[e] = others * __builtin_amdgcn_exp2f(fmaf(u.at(e), a.scale, -lse) * kLog2e);
                 if (c0 + e == target) d[e] = own;
             }
         }
@@ -330,8 +347,10 @@ template <class T, int TPR, bool XENT>
 void launch_bwd(const LogpArgs& a, float* loss, hipStream_t s) {
     dim3 g = grid_of(cdiv(a.rows, 256 / TPR));
     g.z = (unsigned)std::min<int64_t>(cdiv(a.vocab, 16384), 65535);  // along the vocabulary: eight chunks a thread
-    if (past_caches(a, sizeof(T))) logp_bwd_kernel<T, TPR, XENT, true><<<g, 256, 0, s>>>(a, loss);
-    else logp_bwd_kernel<T, TPR, XENT, false><<<g, 256, 0, s>>>(a, loss);
+    const Chunks which = g.z > 1 && a.dlogits == a.logits ? kOthers : kAll;
+    if (past_caches(a, sizeof(T))) logp_bwd_kernel<T, TPR, XENT, true><<<g, 256, 0, s>>>(a, which, loss);
+    else logp_bwd_kernel<T, TPR, XENT, false><<<g, 256, 0, s>>>(a, which, loss);
+    if (which == kOthers) logp_bwd_kernel<T, 8, XENT, false><<<grid_of(cdiv(a.rows, 32)), 256, 0, s>>>(a, kTargets, loss);
 }
 // A team about as wide as a row: 165000 rows of 128 bf16 16 us with 8 threads a row, 122 with 256; 50000 of 1024 34 with
 // 32 and 50.

@@ -72,3 +72,46 @@ def test_pref_of_long_answers_keeps_its_bits(n, apart, beta, smooth, mean):
         _near("reward", _np(reward), wr, (1 + 2 ** -8) * F * abs(wr) + off)
         _near("loss", _np(loss), wl, (1 + 2 ** -8) * F * wl + off * wl)
         _near("dlogp", _np(d), wd, (1 + 2 ** -8) * F * abs(wd) + off * size)
+
+
+# ------------------------------------------------------------------ log probabilities
+@pytest.mark.parametrize("rows,vocab,shift", [(50, 100, 3e4), (40, 700, -1e5), (20, 1024, 3e4), (12, 3000, 1e5),
+                                              (6, 20000, -1e5), (3, 50000, 1e5), (4, 70001, 1e5), (6, 3, -3e4)])
+def test_logp_gradient_of_far_logits(rows, vocab, shift):
+    """Logits far from 0: the gradient is as exact as near 0.  lse is rounded to fp32, by up to |lse| F, and logp keeps
+    what that loses.  A term p's exponent x = z - lse is off by F of itself for each of four operations, logp by its own
+    bound (the forward tests': c and 4 F of its parts) and by F of itself on its way; the rest are some 24 operations."""
+    torch = torch_cuda()
+    announce(f"gradient of far logits, {rows} x {vocab}, around {shift}")
+    x = _normal(rows, rows, vocab, scale=2.5)
+    t = np.random.default_rng(vocab).integers(0, vocab, rows)
+    at = torch.arange(rows), torch.from_numpy(t)
+    x[at] += torch.tensor([0.0, 6.0, 15.0], device="cuda").repeat(rows)[:rows]
+    x += shift
+    targets, g = _i32(t.tolist()), _normal(5, rows)
+    logp, lse = torch.full((2, rows), NAN, device="cuda")
+    ws = _ws(A.fo_logp_workspace(rows, vocab))
+    for scale in (1.0, 0.8):
+        A.fo_logp_fwd(x, targets, logp, lse, scale=scale, workspace=ws)
+        sc, z = float(np.float32(scale)), _np(x)
+        lp, ls, p, miss, _, _ = R.logp(z, t, sc)
+        d = torch.full_like(x, NAN)
+        A.fo_logp_bwd(x, targets, logp, lse, g, d, scale=scale)
+        want = R.logp_grad(z, t, sc, _np(g))
+        spread = sc * (z.max(1) - z.min(1))
+        c = (64 + vocab / 1024 + 3 * spread) * F
+        gap = sc * (z.max(1) - z[np.arange(rows), t])
+        own_off = c * miss + 4 * F * (abs(lp) + (gap > 0) * (gap + np.log(vocab) + 1))
+        far = abs(sc * z - ls[:, None])
+        bound = abs(want) * ((1 + 24) * F + 4 * F * far + (own_off + 2 * F * abs(lp))[:, None])
+        bound[np.arange(rows), t] += abs(sc * _np(g)) * own_off
+        _near("dlogits", _np(d), want, bound)
+        e, loss = torch.full_like(x, NAN), torch.empty(rows, device="cuda")
+        A.fo_xent(x, targets, -g, loss, e, scale=scale, workspace=ws)
+        _near("dlogits of the loss", _np(e), want, bound)
+        over = x.clone()
+        A.fo_logp_bwd(over, targets, logp, lse, g, over, scale=scale)
+        assert torch.equal(over, d)
+        over = x.clone()
+        A.fo_xent(over, targets, -g, loss, over, scale=scale, workspace=ws)
+        assert torch.equal(over, e)
