@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(256) gemm_f8_join_kernel(GemmF8Args g, const f
 // memory's latency for themselves, and a lone tile of 128 is shared by eight waves (600 x 4096 x 4096 21.3 us with
 // four).  From two rounds of workgroups on, two stages and two workgroups a CU hide it better.
 constexpr int kCUs = 256;
-bool few_rows(const GemmF8Args& g) { return g.M <= 16 || (g.M <= 32 && cdiv(g.N, 64) < kCUs); }
+bool few_rows(int64_t M, int32_t N) { return M <= 16 || (M <= 32 && cdiv(N, 64) < kCUs); }
 // Slices of k, of 2048 or more, where 64 x 64 tiles are few and k is long: 100 x 1024 x 8192 14.2 -> 11.8 us, 40 x 512 x
 // 16384 23.6 -> 10.9; the launch that joins them eats the gain up where k is shorter (256 x 256 x 4096 9.2 -> 9.9).
 int slices_of(int64_t M, int32_t N, int32_t K) {
@@ -480,7 +480,7 @@ fo_status run(const GemmF8Args& g, char* ws, hipStream_t s) {
     const bool whole = g.K % 16 == 0 && g.lda < kTileStride && g.ldb < kTileStride && g.lda % 16 == 0 &&
                        g.ldb % 16 == 0 && ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0;
     const int64_t ld = cdiv(g.K, 16) * 16;
-    if (few_rows(g)) {
+    if (few_rows(g.M, g.N)) {
         const dim3 grid = grid_of(cdiv(g.N, 16));
         // eight waves share k where columns are few (4 x 4096 x 4096: 6.5 us either way), else four (1 x 128000 x 4096:
         // 88 us, 108 with eight)
@@ -508,10 +508,10 @@ fo_status run(const GemmF8Args& g, char* ws, hipStream_t s) {
 }  // namespace
 
 int64_t gemm_f8_workspace(int64_t M, int32_t N, int32_t K) {
-    if (!M) return 0;
+    if (few_rows(M, N)) return 0;  // no rows among them
     const int64_t ld = cdiv(K, 16) * 16;
-    if (!copies_pay(M, N, K)) return part_bytes(M, N, K);
-    return part_bytes(M, N, (int32_t)ld) + (M + N) * ld;
+    if (copies_pay(M, N, K)) return part_bytes(M, N, (int32_t)ld) + (M + N) * ld;
+    return K % 16 ? 0 : part_bytes(M, N, K);  // odd rows go to the kernel for any operands
 }
 
 fo_status launch_gemm_f8(int32_t dtype, const GemmF8Args& g, void* ws, hipStream_t s) {

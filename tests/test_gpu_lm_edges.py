@@ -115,3 +115,18 @@ def test_logp_gradient_of_far_logits(rows, vocab, shift):
         over = x.clone()
         A.fo_xent(over, targets, -g, loss, over, scale=scale, workspace=ws)
         assert torch.equal(over, e)
+
+
+# ------------------------------------------------------------------ 8-bit product
+def test_gemm_f8_without_a_workspace():
+    """As its workspace call says: few rows, long k and odd k among them, and a small product of odd rows."""
+    torch = torch_cuda()
+    for M, N, K in ((4, 4096, 8192), (16, 64, 65536), (32, 512, 16400), (7, 100, 9001), (40, 100, 9001)):
+        announce(f"8-bit product without a workspace, {M} x {N} x {K}")
+        assert A.fo_gemm_f8_workspace(M, N, K) == 0
+        v = R.f8_values()
+        a, b = (np.random.default_rng(n).integers(0, 0x7F, (n, K)).astype(np.uint8) for n in (M, N))
+        c = torch.empty((M, N), device="cuda")
+        A.fo_gemm_f8(torch.from_numpy(a).cuda(), None, torch.from_numpy(b).cuda(), None, c)
+        want, size = R.gemm(v[a], None, v[b], None)
+        _near("c", _np(c), want, HALF["f32"] * abs(want) + (K + 4) * F * size)
