@@ -121,14 +121,16 @@ __global__ void __launch_bounds__(S::THREADS) norm_kernel(NormArgs a) {
 #pragma unroll
     for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ss += h[c][e] * h[c][e];
-            top = fmaxf(top, fabsf(OUT == kQuantF8 ? h[c][e] : h[c][e] * w[c][e]));
-        }
+        for (int e = 0; e < 8; ++e) ss += h[c][e] * h[c][e];
     float r = 1.f;
     if (OUT != kQuantF8) r = rstd_of(team<S::TPR>(ss, lds, Add()), a.cols, a.eps);
+    // the largest of y itself: h w may leave fp32's range where y does not
+#pragma unroll
+    for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(OUT == kQuantF8 ? h[c][e] : h[c][e] * r * w[c][e]));
     float2 f8 = make_float2(0.f, 0.f);
-    if (OUT != kNorm) f8 = f8_scale(team<S::TPR>(top, lds + 16, Max()) * r);
+    if (OUT != kNorm) f8 = f8_scale(team<S::TPR>(top, lds + 16, Max()));
     if (t == 0) {
         if (OUT == kNorm && a.rstd) a.rstd[row] = r;
         if (OUT != kNorm) a.y_scale[row] = f8.x;
@@ -155,7 +157,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(NormArgs a) {
     __shared__ float lds[32];
     const int64_t row = block_of();
     if (row >= a.rows) return;
-    float ss = 0.f, top = 0.f;
+    float ss = 0.f;
+    double top = 0.0;  // |h w| before the row's factor is known: within range in 64 bits
     for (int64_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += 8192) {
         const int n = (int)min((int64_t)8, a.cols - c0);
         float h[8], w[8];
@@ -164,13 +167,13 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             ss += h[e] * h[e];
-            top = fmaxf(top, fabsf(OUT == kNormF8 ? h[e] * w[e] : h[e]));
+            top = fmax(top, fabs(OUT == kNormF8 ? (double)h[e] * w[e] : (double)h[e]));
         }
     }
     float r = 1.f;
     if (OUT != kQuantF8) r = rstd_of(team<1024>(ss, lds, Add()), a.cols, a.eps);
     float2 f8 = make_float2(0.f, 0.f);
-    if (OUT != kNorm) f8 = f8_scale(team<1024>(top, lds + 16, Max()) * r);
+    if (OUT != kNorm) f8 = f8_scale(team<1024>((float)(top * r), lds + 16, Max()));
     if (threadIdx.x == 0) {
         if (OUT == kNorm && a.rstd) a.rstd[row] = r;
         if (OUT != kNorm) a.y_scale[row] = f8.x;

@@ -117,6 +117,25 @@ def test_logp_gradient_of_far_logits(rows, vocab, shift):
         assert torch.equal(over, e)
 
 
+# ------------------------------------------------------------------ 8-bit rows
+@pytest.mark.parametrize("h,w,eps", [(1e-17, 1e-29, 0.0), (1e-3, 1e-25, 1e-6), (1e-16, 1e26, 0.0), (1e15, 1e27, 1e-6),
+                                     (1e15, 1e-25, 0.0)])
+@pytest.mark.parametrize("cols", [90, 5003, 33001])
+def test_norm_f8_of_far_operands(cols, h, w, eps):
+    """h and w whose product leaves fp32's range, or its full precision, where y does not.  Tolerances: the 8-bit rows'
+    of the other tests."""
+    torch = torch_cuda()
+    from tests.test_gpu_lm_ops import _check_f8, _norm_slack
+    for dtype in (torch.float32, torch.bfloat16):
+        announce(f"8-bit norm, h {h}, w {w}, {cols} columns, {dtype}")
+        x, wt = (_normal(1, 5, cols) * h).to(dtype), ((1 + 0.3 * _normal(2, cols)) * w).to(dtype)
+        q, s = torch.empty((5, cols), dtype=torch.uint8, device="cuda"), torch.empty(5, device="cuda")
+        A.fo_rmsnorm_f8(x, wt, q, s, eps)
+        y = R.rmsnorm(_np(x), None, _np(wt), float(np.float32(eps)))[2]
+        assert (abs(y).max(1) > 2.0 ** -100).all()
+        _check_f8(y, q.cpu().numpy(), _np(s), _norm_slack(cols))
+
+
 # ------------------------------------------------------------------ 8-bit product
 def test_gemm_f8_without_a_workspace():
     """As its workspace call says: few rows, long k and odd k among them, and a small product of odd rows."""
