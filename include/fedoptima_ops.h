@@ -251,9 +251,8 @@ FO_API fo_status fo_logp_fwd(int32_t dtype, int64_t rows, int32_t vocab, const v
                              int64_t workspace_bytes, void* hip_stream);
 
 /* dlogits_v = scale dlogp[r] (1{v = t} - exp(z_v - lse)), logp and lse as the
- * forward call left them, lse finite or -infinity (scale logits within fp32).  Every
- * row is written (zeros where it is ignored; its dlogp is not read).  dlogits may be
- * logits, with its row stride. */
+ * forward call left them.  Every row is written (zeros where it is ignored; its
+ * dlogp is not read).  dlogits may be logits, with its row stride. */
 FO_API fo_status fo_logp_bwd(int32_t dtype, int64_t rows, int32_t vocab, const void* logits, int64_t ld,
                              const int32_t* targets, float scale, const float* logp, const float* lse,
                              const float* dlogp, void* dlogits, int64_t dlogits_ld, void* hip_stream);

@@ -195,11 +195,14 @@ __global__ void __launch_bounds__(64) logp_join_kernel(LogpArgs a, const Part* _
 // target's logit before it has read it: all but its chunk in one launch, that chunk in the next.
 enum Chunks { kAll, kOthers, kTargets };
 
-// exp(z - lse) of every term is off by what lse lost when it was rounded, up to |lse| 2^-24 of itself: as long as logp is
-// the smaller of the two, z_t - logp says how much that was, to 2^-24 |logp| (logits around 100000: gradients off by
-// 3e-3, and by 1e-6 so).  One factor a row.
-__device__ __forceinline__ float lost_of(float zt, float scale, float logp, float lse) {
-    return fabsf(logp) < fabsf(lse) && lse - lse == 0.f ? expf(logp - fmaf(zt, scale, -lse)) : 1.f;
+// scale (u - from) + at = z - lse.  By lse every term is off by what lse lost when it was rounded, up to |lse| 2^-24 of
+// itself (logits around 100000: 3e-3); by the target's logit and logp, whose difference lse is, up to 2 |logp| 2^-24 where
+// the terms are large.  No lse is too large for that, nor infinite where scale takes the maximum past fp32.
+struct Origin {
+    float from, at;
+};
+__device__ __forceinline__ Origin origin(float zt, float logp, float lse) {
+    return 2.f * fabsf(logp) < fabsf(lse) ? Origin{zt, logp} : Origin{0.f, -lse};
 }
 
 // XENT: weight is minus the gradient by logp, and logp becomes the loss.  NT: past the caches.
@@ -218,7 +221,8 @@ __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, Chunks which,
     if (XENT && which != kTargets && blockIdx.z == 0 && t == 0) loss[row] = there ? -logp : 0.f;
     const bool none = !there || lse == -INFINITY;
     const float g = none ? 0.f : (XENT ? -a.weight[row] : a.weight[row]) * a.scale;
-    const float own = none ? 0.f : g * -expm1f(logp), others = none ? 0.f : -g * lost_of(zt, a.scale, logp, lse);
+    const float own = none ? 0.f : g * -expm1f(logp);
+    const Origin o = origin(zt, logp, lse);
     const int mine = there ? target >> 3 : -1;
     if (which == kTargets && (t || !there)) return;
     const int first = which == kTargets ? mine : (int)blockIdx.z * TPR + t, last = which == kTargets ? mine + 1 : chunks;
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, Chunks which,
             u.load(x + c0, n, n == 8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                d[e] = others * __builtin_amdgcn_exp2f(fmaf(u.at(e), a.scale, -lse) * kLog2e);
+                d[e] = -g * __builtin_amdgcn_exp2f(fmaf(u.at(e) - o.from, a.scale, o.at) * kLog2e);
                 if (c0 + e == target) d[e] = own;
             }
         }

@@ -117,6 +117,43 @@ def test_logp_gradient_of_far_logits(rows, vocab, shift):
         assert torch.equal(over, e)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+def test_logp_gradient_of_extreme_logits(dtype, scale):
+    """Rows of nothing but a type's lowest value or another far one are uniform; a logit far above the others takes all;
+    one past fp32 with its scale as well.  A uniform row's terms: exp(logp), off by 2 |logp| F and a few operations."""
+    torch = torch_cuda()
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    for vocab in (5, 40, 700, 30000, 70001):
+        announce(f"gradient of extreme logits, {dtype}, {vocab} of them, scale {scale}")
+        x = torch.zeros((6, vocab), dtype=dt, device="cuda")
+        x[0], x[1], x[2] = torch.finfo(dt).min, -1e30, 3e9
+        x[3, 3], x[4, 3], x[5, 4] = 1e10, -1e10, 3e38
+        targets, g = _i32([3, 2, 0, 3, 3, 4]), torch.tensor([1.0, -2.0, 0.5, 1.0, 1.0, 3.0], device="cuda")
+        logp, lse = torch.empty((2, 6), device="cuda")
+        ws = _ws(A.fo_logp_workspace(6, vocab))
+        A.fo_logp_fwd(x, targets, logp, lse, scale=scale, workspace=ws)
+        want = np.zeros((6, vocab))
+        for r in range(3):
+            want[r] = -1.0 / vocab
+            want[r, targets[r].item()] += 1
+        want[4] = -1.0 / (vocab - 1)
+        want[4, 3] = 1
+        want *= float(np.float32(scale)) * _np(g)[:, None]
+        d, e, loss = torch.full_like(x, NAN), torch.full_like(x, NAN), torch.empty(6, device="cuda")
+        A.fo_logp_bwd(x, targets, logp, lse, g, d, scale=scale)
+        bound = abs(want) * (HALF[dtype] * (1 + 2 ** -8) + (4 * np.log(vocab) + 24) * F)
+        _near("dlogits", _np(d), want, bound)
+        A.fo_xent(x, targets, -g, loss, e, scale=scale, workspace=ws)
+        _near("dlogits of the loss", _np(e), want, bound)
+    x = torch.zeros((1, 40), dtype=dt, device="cuda")
+    x[0, 4] = 3e38
+    A.fo_logp_fwd(x, _i32([4]), logp[:1], lse[:1], scale=4.0)
+    d = torch.full_like(x, NAN)
+    A.fo_logp_bwd(x, _i32([4]), logp[:1], lse[:1], g[:1], d, scale=4.0)
+    assert float(logp[0]) == 0 and (d == 0).all()
+
+
 # ------------------------------------------------------------------ 8-bit rows
 @pytest.mark.parametrize("h,w,eps", [(1e-17, 1e-29, 0.0), (1e-3, 1e-25, 1e-6), (1e-16, 1e26, 0.0), (1e15, 1e27, 1e-6),
                                      (1e15, 1e-25, 0.0)])
