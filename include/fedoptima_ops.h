@@ -220,7 +220,7 @@ FO_API fo_status fo_quant_f8(int32_t dtype, int64_t rows, int32_t cols, const vo
 
 /* c_mn = a_scale[m] b_scale[n] sum_k a_mk b_nk, a [M][K] and b [N][K] in 8 bits,
  * summed in fp32 and rounded once to dtype.  a_scale [M] and b_scale [N] may be
- * NULL (ones).  M >= 0; N, K >= 1.  In bf16 calls the products enter those sums by
+ * NULL (ones); the sum is multiplied by a_scale first, in fp32.  M >= 0; N, K >= 1.  In bf16 calls the products enter those sums by
  * eights, each cut below 2^-13 of the largest of its eight (the 8-bit matrix
  * instruction's way: some 1.4e-5 of the result's norm); fp32 calls keep all bits of
  * the products and take about twice as long.  Rows that start 16-byte aligned with

@@ -61,7 +61,7 @@ fo_status check_workspace(const char* what, const void* ws, int64_t bytes, int64
     } while (0)
 
 // ------------------------------------------------------------------ embedding
-// 128 columns a workgroup in a launch's third dimension; 4096 rows a tile of the sort.
+// 128 columns a workgroup in a launch's third dimension; tiles of the sort of 1024 rows, of 4096 above 2^20 rows.
 constexpr int32_t kMaxEmbedCols = 1 << 22;
 constexpr int64_t kMaxEmbedRows = int64_t(1) << 28;
 

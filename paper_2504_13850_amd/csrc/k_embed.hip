@@ -7,8 +7,8 @@
 // atomics on them: the rows are sorted by token (stable), the sorted list is cut
 // into pieces of equal length whatever the tokens are, a team of threads sums a
 // piece's rows and writes each token that begins and ends inside it, and the sums of
-// tokens that cross pieces are joined by a last launch.  The zeros are written beside
-// the first launch of the sort, which leaves the memory idle.
+// tokens that cross pieces are joined by a last launch.  The zeros are written in
+// shares beside the sort's launches, which leave the memory idle.
 #include <algorithm>
 
 #include "lm.h"
@@ -305,8 +305,9 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_place_kernel(EmbedArgs a, 
 }
 
 // ------------------------------------------------------------------ sums
-// Entries of a piece: short pieces where rows are few or narrow, so that teams fill the chip, and some thousand pieces at
-// most, for each takes a workgroup of the join (the gradient, bf16: 56548 rows of 101 in pieces of 16 35 us, of 64 54;
+// Entries of a piece: short pieces where rows are few or narrow, so that teams fill the chip.  Each piece takes a
+// workgroup of the join, so pieces grow up to 64 entries, which keeps some thousand of them up to 100000 or 260000 rows;
+// with more rows there are more, one for 64 rows (the gradient, bf16: 56548 rows of 101 in pieces of 16 35 us, of 64 54;
 // 65536 of 2048 197 and 187, of 768 69 and 63; 200000 of 128 76 and 50).
 int piece_of(int64_t rows, int32_t cols) {
     const int64_t most = 256 >> team_bits(cols) >= 8 ? 4096 : 1536;

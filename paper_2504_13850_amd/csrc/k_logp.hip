@@ -3,7 +3,7 @@
 // Bound by HBM: the logits are read once (forward), read and written once
 // (gradient; cross-entropy where a row lies in the registers of a workgroup).
 // 8192 rows of 32000 bf16, a tenth without a target, cross-entropy: 167 us, 6.0
-// TB/s; forward and gradient of 5565 such rows 176 us, 6.1 TB/s (a copy of a GiB
+// TB/s; forward and gradient of 5565 such rows 178 us, 6.0 TB/s (a copy of a GiB
 // runs at 5.15).  Some ten instructions a logit and pass, the exponential at a
 // quarter of the rate: half of that time, hidden where loads are not held up.
 // Running maximum and sum leave the target's term out: with it, 1 - p and log p
@@ -245,7 +245,8 @@ __global__ void __launch_bounds__(256) logp_bwd_kernel(LogpArgs a, Chunks which,
 
 // Cross-entropy with the row in registers: maximum and sum of what is held, then the gradient from it.  64 registers,
 // two workgroups of 1024 on a CU, where a thread holds four chunks: one works while the other waits (8192 rows of 32000
-// bf16 177 us, 224 with one).  NT: the gradient past the caches.
+// bf16 177 us, 224 with one).  Left alone the compiler takes 70 for four chunks, 56 for three, which fits without being
+// told, and 83 for six, which never would.  NT: the gradient past the caches.
 template <class T, int TPR, int NC, bool NT>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR * NC == 4096 ? 8 : 4) xent_kernel(LogpArgs a) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, RPW = THREADS / TPR;

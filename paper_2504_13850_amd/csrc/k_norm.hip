@@ -218,8 +218,8 @@ fo_status fwd_any(NormOut out, const NormArgs& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ backward
-// Columns that the registers of a workgroup hold with the weight's gradient (3000 rows of 20000 bf16: 161 us through the
-// long rows' kernels, 320 with what spills; fp32, 2000 rows without residual: 188 and 316).
+// Columns that the registers of a workgroup hold with the weight's gradient (3000 rows of 20000 bf16: 153 us through the
+// long rows' kernels, 320 with what spills; fp32, 2000 rows without residual: 192 and 316).
 constexpr int64_t kBwdCols = Shape<1024, 1024, 2>::COLS;
 
 // Workgroups, and parts of the weight's gradient: each takes every so many-th row.  As many as the chip has room for:
