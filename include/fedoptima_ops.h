@@ -279,10 +279,11 @@ FO_API fo_status fo_xent(int32_t dtype, int64_t rows, int32_t vocab, const void*
  * rows has reward 0.  logp, ref, dlogp: device fp32[rows]; begin, end: device
  * int32[2 pairs], clamped to the rows; loss fp32[pairs], reward fp32[2 pairs].  No
  * two answers share rows.  Rows of no answer are neither read nor written.  dlogp
- * (may be NULL) may be logp.  Computed in fp64 and rounded once.  beta finite, smooth in [0, 1].  An
- * infinite reward (a token of probability 0) gives the loss's limit, infinity or,
- * where the growing term has no weight, 0, and a finite gradient; two of the same
- * infinity, and an infinity times beta = 0, give NaN in their pair.
+ * (may be NULL) may be logp.  Computed in fp64 and rounded once.  beta finite,
+ * smooth in [0, 1].  An infinite reward (a token of probability 0) gives the loss's
+ * limit, infinity or, where the growing term has no weight, 0, and a finite
+ * gradient; two of the same infinity, and an infinity times beta = 0, give NaN in
+ * their pair.
  * Errors: FO_EINVAL, FO_EHIP. */
 FO_API fo_status fo_pref_loss(int32_t pairs, int64_t rows, const int32_t* begin, const int32_t* end, const float* logp,
                               const float* ref, float beta, float smooth, int32_t mean, float dloss, float* loss,
